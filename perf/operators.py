@@ -5,9 +5,9 @@
               renormalised and scaled weights), with counts, offsets and the stable order by expert
 ``norm``      ``binding.norm_residual``: the norm behind a block, its gate, the residual scale, the
               residual addition and the norm in front of the next block
-``product``   ``binding.matmul_fp8_block``: a matrix product of e4m3 codes, one fp32 scale per row
+``product``   ``binding.matmul_blocks``: a matrix product of e4m3 codes, one fp32 scale per row
               and 128 columns of the left operand and per 128 x 128 block of the right one
-``quantize``  ``binding.quantize_fp8_block``: bf16 rows, or SwiGLU of rows, to codes and scales
+``quantize``  ``binding.quantize_blocks``: bf16 rows, or SwiGLU of rows, to codes and scales
 
 ``run`` computes them in elementary torch operations, or, where ``own`` is true, with the library.
 """
@@ -332,12 +332,12 @@ def _own(s):
             s["shape"] = binding.ProductShape(n=c["n"], k=c["k"], out=binding.FP32 if c["out"] == "fp32" else binding.BF16,
                                               a_stride=c["k"], a_scale_stride=kb, b_stride=c["k"], b_scale_stride=kb,
                                               add_stride=c["n"], out_stride=c["n"])
-        rc = binding.matmul_fp8_block(s["shape"], s["a"].data_ptr(), s["a_scale"].data_ptr(), s["b"].data_ptr(),
+        rc = binding.matmul_blocks(s["shape"], s["a"].data_ptr(), s["a_scale"].data_ptr(), s["b"].data_ptr(),
                                       s["b_scale"].data_ptr(), _ptr(s["add"]), c["m"], stream, s["out"].data_ptr())
         got = s["out"]
     else:
         k = c["cols"]
-        rc = binding.quantize_fp8_block(s["x"].data_ptr(), s["x"].shape[1], c["rows"], k, 1 if c["swiglu"] else 0, stream,
+        rc = binding.quantize_blocks(s["x"].data_ptr(), s["x"].shape[1], c["rows"], k, 1 if c["swiglu"] else 0, stream,
                                         s["codes"].data_ptr(), k, s["scales"].data_ptr(), -(-k // BLOCK))
         got = {"codes": s["codes"], "scales": s["scales"]}
     if rc != 0:
