@@ -369,6 +369,96 @@ int oled_route_noalloc(const void* hidden, const void* w_router, const float* bi
                        int32_t n_experts, int32_t top_k, void* cuda_stream, int32_t* ids,
                        float* gate, int32_t* counts, int32_t* offsets, int32_t* perm);
 
+/* ---- operators around the routed experts ----------------------------------------------------------
+ * What an MoE layer of a served model has next to its routed experts.  Each call works on device memory of the
+ * current device that the caller owns, is enqueued on cuda_stream (a stream of that device) and needs no context; the library allocates
+ * nothing and keeps nothing between calls, so calls may overlap, be captured and be replayed in any order, provided
+ * that they write different arrays.  Rows may lie further apart than they are long (strides count elements; what lies
+ * between rows is neither read nor written); arrays that a call writes may overlap nothing else that it is given,
+ * unless said otherwise.  Every argument is checked before anything is launched (INVALID_ARG); no rows at all is no error. */
+#define OLED_BF16 0
+#define OLED_FP32 1
+#define OLED_MAX_PRODUCT_K 16384   /* columns of a row of codes */
+#define OLED_MAX_ROUTE_TOKENS (1 << 20)
+
+/* Routing of n_tokens tokens from their gate logits (fp32).
+ *   score  s_e = 1 / (1 + exp(-l_e)), or the softmax of the token's logits.
+ *   choice s_e + bias_e (a bias that balances the experts' loads; it takes no part in the weights), without a bias l_e itself.
+ *   groups consecutive experts; a group counts as its largest choice (group_top 1) or as the sum of its two largest
+ *          s_e + bias_e (2), and the token's experts come from the top_groups largest groups.
+ *   ids    the top_k largest choices, in descending order.  Equal values go to the lower index.  Choices are told apart as
+ *          in 64-bit arithmetic, whatever the speed of the scores' own precision would suggest.
+ *   gate   scale * s / (sum of the chosen s + 1e-20) with renormalise, else scale * s.
+ * A NaN logit counts as -inf, its choice and a choice that is NaN too; the ids of a token stay distinct, also where every
+ * choice is -inf. */
+#define OLED_SCORE_SOFTMAX 0
+#define OLED_SCORE_SIGMOID 1
+typedef struct {
+  int32_t n_experts;   /* 1 .. OLED_MAX_EXPERTS */
+  int32_t top_k;       /* 1 .. OLED_MAX_TOPK, at most the experts of top_groups groups */
+  int32_t score;       /* OLED_SCORE_* */
+  int32_t n_groups;    /* 1 .. 32, a divisor of n_experts; 1: no groups */
+  int32_t top_groups;  /* 1 .. n_groups */
+  int32_t group_top;   /* 1 or 2 (groups of two experts and more) */
+  int32_t renormalise; /* 0 or 1 */
+  float scale;
+} oled_routing;
+/*   logits fp32[n_tokens] rows of n_experts, logits_stride apart; bias fp32[n_experts] or NULL.
+ *   ids int32[n_tokens*top_k], gate fp32[n_tokens*top_k]; counts int32[n_experts], offsets int32[n_experts+1] and
+ *   perm int32[n_tokens*top_k] (the stable order by expert) as oled_route_noalloc() gives them, or all three NULL.
+ *   scratch: oled_route_scored_scratch() bytes of device memory (0 bytes up to 4096 assignments: may be NULL),
+ *   used until the enqueued work completes; only the order by expert needs it.
+ * n_tokens at most OLED_MAX_ROUTE_TOKENS, else TOO_MANY_TOKENS.  All arrays 4-byte aligned. */
+int oled_route_scored(const oled_routing* routing, const float* logits, int64_t logits_stride, const float* bias,
+                      int32_t n_tokens, void* cuda_stream, int32_t* ids, float* gate, int32_t* counts, int32_t* offsets,
+                      int32_t* perm, void* scratch, size_t scratch_bytes);
+size_t oled_route_scored_scratch(const oled_routing* routing, int32_t n_tokens);
+
+/* The norms around a block with its gate and residual, in one pass:
+ *   z  = rms(y) * post_weight   (post_weight NULL: z = y)
+ *   x_out = x + residual_scale * gate * z   (gate NULL: 1; y NULL: x_out = x)
+ *   h  = rms(x_out) * pre_weight, as bf16 (h), as e4m3 codes with a scale per row and 128 columns (h_codes, h_scales;
+ *        as oled_quantize_blocks() makes them), both, or, with pre_weight NULL, not at all
+ *   rms(v) = v / sqrt(mean(v^2) + eps)
+ * Computed in fp32; h is made from the unrounded x_out.  x, y: [n_tokens, hidden]; x and x_out in `residual`'s type, all else bf16.
+ * gate: one row for every gate_tokens consecutive tokens (a gate per block of a batch), or one for all of them (0).
+ * x_out may be NULL.  x_out and h may each be x or y itself (the same address, stride and type). */
+typedef struct {
+  int32_t hidden;       /* 1 .. 16384 */
+  int32_t residual;     /* OLED_BF16 or OLED_FP32: type of x and x_out */
+  int32_t gate_tokens;
+  float eps;            /* > 0 */
+  float residual_scale;
+  int64_t x_stride, y_stride, gate_stride, x_out_stride, h_stride, codes_stride, scales_stride;
+} oled_norm_shape;
+int oled_norm_residual(const oled_norm_shape* shape, const void* x, const void* y, const void* post_weight,
+                       const void* gate, const void* pre_weight, int32_t n_tokens, void* cuda_stream, void* x_out, void* h,
+                       void* h_codes, float* h_scales);
+
+/* Rows of bf16 values as e4m3 codes with one fp32 scale per row and 128 columns (the last block may be shorter): scale = amax / 448,
+ * code = e4m3(value * (448 / amax)), with amax the block's largest magnitude, at least 2^-100.  swiglu = 1: a row of x
+ * holds 2 * cols values, gate | up, and the value is silu(gate) * up in fp32.  An infinity or a NaN in a block makes
+ * every value of the block read as NaN.
+ *   x: [rows, cols or 2 cols] bf16, 16-byte aligned rows (x_stride a multiple of 8); cols a multiple of 16, at most OLED_MAX_PRODUCT_K.
+ *   codes: [rows, cols] bytes, 16-byte aligned rows (codes_stride a multiple of 16); scales fp32 [rows, ceil(cols / 128)]. */
+int oled_quantize_blocks(const void* x, int64_t x_stride, int32_t rows, int32_t cols, int32_t swiglu, void* cuda_stream,
+                            void* codes, int64_t codes_stride, float* scales, int64_t scales_stride);
+
+/* out[m, n] = sum_k (a[m, k] * a_scale[m, k / 128]) * (b[n, k] * b_scale[n / 128, k / 128]) (+ add[m, n]): the products of a dense
+ * expert, of e4m3 codes.  Accumulated in fp32, rounded once.
+ *   a: [m, k] codes, b: [n, k] codes; 16-byte aligned rows (strides multiples of 16), k a multiple of 16, at most OLED_MAX_PRODUCT_K.
+ *   a_scale fp32 [m, ceil(k / 128)], b_scale fp32 [ceil(n / 128), ceil(k / 128)]; a product of two scales has to be a normal
+ *   number.  A code that is NaN makes its row (of a) or column (of b) NaN.
+ *   add: [m, n] bf16 or NULL, may be out itself.  out: [m, n] in `out`'s type.  m at most OLED_MAX_ROUTE_TOKENS (TOO_MANY_TOKENS).
+ * Should a device-side wait run out (2 s), the tile's results are NaN. */
+typedef struct {
+  int32_t n, k;         /* n at most 2^20 */
+  int32_t out;          /* OLED_BF16 or OLED_FP32 */
+  int64_t a_stride, a_scale_stride, b_stride, b_scale_stride, add_stride, out_stride;
+} oled_product_shape;
+int oled_matmul_blocks(const oled_product_shape* shape, const void* a, const float* a_scale, const void* b,
+                          const float* b_scale, const void* add, int32_t m, void* cuda_stream, void* out);
+
 /* ---- host-only policy simulator (no GPU needed): the same C++ policy code the step uses,
  * driven by recorded counts and integer scores.  For tests of the host logic. ---- */
 typedef struct oled_policy oled_policy;

@@ -46,10 +46,14 @@ EXPORTS = [
     "oled_adapt_capacity", "oled_get_capacity", "oled_policy_set_policy", "oled_policy_fills_reused",
     "oled_policy_adapt", "oled_clear_status", "oled_policy_time", "oled_expert_blob_bytes",
     "oled_self_check_report", "oled_debug_perm", "oled_policy_create_stack", "oled_debug_timeline",
-    "oled_policy_tile_rows",
+    "oled_policy_tile_rows", "oled_route_scored", "oled_route_scored_scratch", "oled_norm_residual",
+    "oled_quantize_blocks", "oled_matmul_blocks",
 ]
 EXPERTS_BF16, EXPERTS_FP8 = 0, 1
 NOALLOC_MAX_TOKENS = 256
+BF16, FP32 = 0, 1
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+MAX_PRODUCT_K, MAX_ROUTE_TOKENS = 16384, 1 << 20
 
 
 class ModelShape(C.Structure):
@@ -57,6 +61,29 @@ class ModelShape(C.Structure):
                 ("top_k", C.c_int32), ("intermediate", C.c_int32), ("max_tokens", C.c_int32),
                 ("has_router_bias", C.c_int32), ("staging_slots", C.c_int32),
                 ("expert_format", C.c_int32)]
+
+
+class Routing(C.Structure):
+    """``oled_routing``."""
+    _fields_ = [(n, C.c_int32) for n in ("n_experts", "top_k", "score", "n_groups", "top_groups", "group_top",
+                                         "renormalise")] + [("scale", C.c_float)]
+
+    def __init__(self, n_experts: int, top_k: int, score: int = SCORE_SOFTMAX, n_groups: int = 1, top_groups: int = 1,
+                 group_top: int = 1, renormalise: int = 1, scale: float = 1.0):
+        super().__init__(n_experts, top_k, score, n_groups, top_groups, group_top, renormalise, scale)
+
+
+class NormShape(C.Structure):
+    """``oled_norm_shape``; strides count elements."""
+    _fields_ = [("hidden", C.c_int32), ("residual", C.c_int32), ("gate_tokens", C.c_int32), ("eps", C.c_float),
+                ("residual_scale", C.c_float)] + [(n, C.c_int64) for n in (
+                    "x_stride", "y_stride", "gate_stride", "x_out_stride", "h_stride", "codes_stride", "scales_stride")]
+
+
+class ProductShape(C.Structure):
+    """``oled_product_shape``; strides count elements."""
+    _fields_ = [("n", C.c_int32), ("k", C.c_int32), ("out", C.c_int32)] + [(n, C.c_int64) for n in (
+        "a_stride", "a_scale_stride", "b_stride", "b_scale_stride", "add_stride", "out_stride")]
 
 
 class KernelProfile(C.Structure):
@@ -147,6 +174,13 @@ def load() -> C.CDLL:
     lib.oled_policy_tile_rows.argtypes = [i32, i32, i32, i32, i32]
     lib.oled_policy_adapt.argtypes = [C.POINTER(vp), i32, i32, vp]
     lib.oled_route_noalloc.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    i64 = C.c_int64
+    lib.oled_route_scored.argtypes = [C.POINTER(Routing), vp, i64, vp, i32, vp, vp, vp, vp, vp, vp, vp, C.c_size_t]
+    lib.oled_route_scored_scratch.argtypes = [C.POINTER(Routing), i32]
+    lib.oled_route_scored_scratch.restype = C.c_size_t
+    lib.oled_norm_residual.argtypes = [C.POINTER(NormShape), vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp]
+    lib.oled_quantize_blocks.argtypes = [vp, i64, i32, i32, i32, vp, vp, i64, vp, i64]
+    lib.oled_matmul_blocks.argtypes = [C.POINTER(ProductShape), vp, vp, vp, vp, vp, i32, vp, vp]
     _lib = lib
     return lib
 
@@ -326,6 +360,37 @@ def route_noalloc(hidden_ptr, w_router_ptr, bias_ptr, conf_ptr, n_tokens: int, h
     return load().oled_route_noalloc(hidden_ptr, w_router_ptr, bias_ptr, conf_ptr, n_tokens, hidden,
                                      n_experts, top_k, C.c_void_p(cuda_stream), ids_ptr, gate_ptr,
                                      counts_ptr, offsets_ptr, perm_ptr)
+
+
+def route_scored(routing: Routing, logits_ptr, logits_stride: int, bias_ptr, n_tokens: int, cuda_stream: int, ids_ptr,
+                 gate_ptr, counts_ptr, offsets_ptr, perm_ptr, scratch_ptr, scratch_bytes: int) -> int:
+    """``oled_route_scored``: routing from logits.  All pointers are device pointers; returns the status code."""
+    return load().oled_route_scored(routing, logits_ptr, logits_stride, bias_ptr, n_tokens, cuda_stream, ids_ptr, gate_ptr,
+                                    counts_ptr, offsets_ptr, perm_ptr, scratch_ptr, scratch_bytes)
+
+
+def route_scored_scratch(routing: Routing, n_tokens: int) -> int:
+    return int(load().oled_route_scored_scratch(routing, n_tokens))
+
+
+def norm_residual(shape: NormShape, x_ptr, y_ptr, post_weight_ptr, gate_ptr, pre_weight_ptr, n_tokens: int, cuda_stream: int,
+                  x_out_ptr, h_ptr, h_codes_ptr, h_scales_ptr) -> int:
+    """``oled_norm_residual``: the norms around a block, its gate and residual.  Returns the status code."""
+    return load().oled_norm_residual(shape, x_ptr, y_ptr, post_weight_ptr, gate_ptr, pre_weight_ptr, n_tokens, cuda_stream,
+                                     x_out_ptr, h_ptr, h_codes_ptr, h_scales_ptr)
+
+
+def quantize_blocks(x_ptr, x_stride: int, rows: int, cols: int, swiglu: int, cuda_stream: int, codes_ptr,
+                       codes_stride: int, scales_ptr, scales_stride: int) -> int:
+    """``oled_quantize_blocks``: bf16 rows (swiglu: gate | up) to e4m3 codes and scales.  Returns the status code."""
+    return load().oled_quantize_blocks(x_ptr, x_stride, rows, cols, swiglu, cuda_stream, codes_ptr, codes_stride, scales_ptr,
+                                          scales_stride)
+
+
+def matmul_blocks(shape: ProductShape, a_ptr, a_scale_ptr, b_ptr, b_scale_ptr, add_ptr, m: int, cuda_stream: int,
+                     out_ptr) -> int:
+    """``oled_matmul_blocks``: product of e4m3 codes with block scales.  Returns the status code."""
+    return load().oled_matmul_blocks(shape, a_ptr, a_scale_ptr, b_ptr, b_scale_ptr, add_ptr, m, cuda_stream, out_ptr)
 
 
 class PolicySim:

@@ -325,6 +325,20 @@ int launch_ffn_few(cudaStream_t st, const FfnTcMaps& maps, const FfnGroup& grp, 
                    int timeline_slot, const RouteReport& report, uint32_t* done, const TokenSplit* split,
                    uint32_t* split_done, uint32_t* claims);
 
+// ---- operators without a context (norm.cu, quantize.cu, product.cu, route_scored.cu): the entry points' bodies, which
+// check their arguments, and launches that take checked ones ----------------------------------
+int norm_residual(const oled_norm_shape* shape, const void* x, const void* y, const void* post_weight, const void* gate,
+                  const void* pre_weight, int32_t n_tokens, cudaStream_t st, void* x_out, void* h, void* h_codes, float* h_scales);
+cudaError_t launch_quantize(cudaStream_t st, const uint16_t* x, int64_t x_stride, int64_t rows, int cols, bool swiglu,
+                            uint8_t* codes, int64_t codes_stride, float* scales, int64_t scales_stride);
+int matmul_blocks(const oled_product_shape* shape, const void* a, const float* a_scale, const void* b, const float* b_scale,
+                     const void* add, int32_t m, cudaStream_t st, void* out);
+bool routing_valid(const oled_routing* r);
+// The routing of a step from its logits [T,E]; counts, seg_counts (nullptr: none) and scores are raised, as launch_route does.
+cudaError_t launch_route_step(cudaStream_t st, const oled_routing& r, const float* logits, const float* bias, const float* conf,
+                              int T, int32_t* ids, float* gate, int32_t* counts, unsigned long long* scores, int32_t* seg_counts,
+                              int seg_tokens);
+
 // Self-check (check.cu): invariants of the routing and the permutation, guard words.
 void launch_self_check(cudaStream_t st, const int32_t* ids, const int32_t* counts, const int32_t* offsets,
                        const int32_t* perm, const int32_t* pos, int T, int E, int K, uint32_t* status);

@@ -1,0 +1,293 @@
+// The norms around a block, with its gate and residual, in one pass over the rows:
+//   z  = rms(y) * post_weight                        (without post_weight: z = y)
+//   x' = x + residual_scale * gate * z               (without y: x' = x)
+//   h  = rms(x') * pre_weight                        as bf16, and / or as e4m3 codes with a scale per 128 (block_scale.h)
+//   rms(v) = v / sqrt(mean(v^2) + eps)
+// Everything between the loads and the stores is fp32, and every output is rounded once: h is made from x' itself, not
+// from its bf16 form.
+//
+// Bound by HBM (4096 bf16 columns: 8 bytes an element).  A row stays in the registers of one CTA (of one warp up to 256
+// columns) between the two sums that it needs, eight consecutive values per thread and vector, so that sixteen
+// lanes hold a block of 128.
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "block_scale.h"
+#include "kernels.h"
+#include "row_args.h"
+
+namespace oled {
+namespace {
+
+struct NormArgs {
+  const void* x;
+  const uint16_t* y;
+  const uint16_t* post;
+  const uint16_t* gate;
+  const uint16_t* pre;
+  void* x_out;
+  uint16_t* h;
+  uint8_t* codes;
+  float* scales;
+  int64_t x_stride, y_stride, gate_stride, x_out_stride, h_stride, codes_stride, scales_stride;
+  int tokens, hidden, gate_tokens;
+  float eps, scale;
+};
+
+// Eight values at column c of a row, zeros behind its end.  VEC: rows are whole 16-byte vectors on 16-byte boundaries.
+template <bool VEC>
+__device__ __forceinline__ void load8(const uint16_t* row, int c, int hidden, float (&v)[8]) {
+  if (VEC) {
+    uint4 p = make_uint4(0u, 0u, 0u, 0u);
+    if (c < hidden) p = *reinterpret_cast<const uint4*>(row + c);
+    unpack8(p, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < hidden ? __uint_as_float((uint32_t)row[c + j] << 16) : 0.0f;
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void load8(const float* row, int c, int hidden, float (&v)[8]) {
+  if (VEC) {
+    float4 p = make_float4(0.f, 0.f, 0.f, 0.f), q = p;
+    if (c < hidden) {
+      p = *reinterpret_cast<const float4*>(row + c);
+      q = *reinterpret_cast<const float4*>(row + c + 4);
+    }
+    v[0] = p.x; v[1] = p.y; v[2] = p.z; v[3] = p.w;
+    v[4] = q.x; v[5] = q.y; v[6] = q.z; v[7] = q.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < hidden ? row[c + j] : 0.0f;
+  }
+}
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <bool VEC>
+__device__ __forceinline__ void store8(uint16_t* row, int c, int hidden, const float (&v)[8]) {
+  if (VEC) {
+    if (c < hidden)
+      *reinterpret_cast<uint4*>(row + c) =
+          make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (c + j < hidden) row[c + j] = __bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void store8(float* row, int c, int hidden, const float (&v)[8]) {
+  if (VEC) {
+    if (c < hidden) {
+      *reinterpret_cast<float4*>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<float4*>(row + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (c + j < hidden) row[c + j] = v[j];
+  }
+}
+
+// The sum over the THREADS threads of a row (a warp, or the whole CTA), in every one of them.
+template <int THREADS>
+__device__ __forceinline__ float row_sum(float s, float* s_part) {
+#pragma unroll
+  for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+  if (THREADS > 32) {
+    constexpr int kWarps = THREADS / 32;
+    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) s += s_part[w];
+  }
+  return s;
+}
+
+// R: the residual stream's type (uint16_t: bf16).  THREADS per row (32: four rows per CTA), V vectors per thread.
+template <typename R, int THREADS, int V, bool VEC>
+__global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS)
+norm_kernel(const __grid_constant__ NormArgs a) {
+  __shared__ float s_part[2][THREADS / 32];
+  constexpr int kRows = THREADS == 32 ? 4 : 1;
+  const int lane_in_row = (int)threadIdx.x % THREADS, H = a.hidden;
+  const int64_t t = (int64_t)blockIdx.x * kRows + (kRows > 1 ? threadIdx.x / THREADS : 0);
+  griddep_launch_dependents();
+  griddep_wait();
+  if (t >= a.tokens) return;  // (whole warps, and only where no barrier follows)
+  const R* const xr = static_cast<const R*>(a.x) + t * a.x_stride;
+  float v[V][8];
+#pragma unroll
+  for (int i = 0; i < V; ++i) load8<VEC>(xr, (lane_in_row + i * THREADS) * 8, H, v[i]);
+  if (a.y != nullptr) {
+    float z[V][8];
+    const uint16_t* const yr = a.y + t * a.y_stride;
+#pragma unroll
+    for (int i = 0; i < V; ++i) load8<VEC>(yr, (lane_in_row + i * THREADS) * 8, H, z[i]);
+    float f = a.scale;
+    if (a.post != nullptr) {
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s = fmaf(z[i][j], z[i][j], s);
+      const float r = rsqrtf(row_sum<THREADS>(s, s_part[0]) / (float)H + a.eps);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float w[8];
+        load8<VEC>(a.post, (lane_in_row + i * THREADS) * 8, H, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[i][j] = z[i][j] * r * w[j];
+      }
+    }
+    if (a.gate != nullptr) {
+      const uint16_t* const gr = a.gate + (a.gate_tokens > 0 ? t / a.gate_tokens : 0) * a.gate_stride;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float w[8];
+        load8<VEC>(gr, (lane_in_row + i * THREADS) * 8, H, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[i][j] *= w[j];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = fmaf(f, z[i][j], v[i][j]);
+  }
+  if (a.x_out != nullptr) {
+    R* const xo = static_cast<R*>(a.x_out) + t * a.x_out_stride;
+#pragma unroll
+    for (int i = 0; i < V; ++i) store8<VEC>(xo, (lane_in_row + i * THREADS) * 8, H, v[i]);
+  }
+  if (a.pre == nullptr) return;
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s = fmaf(v[i][j], v[i][j], s);
+  const float r = rsqrtf(row_sum<THREADS>(s, s_part[1]) / (float)H + a.eps);
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int c = (lane_in_row + i * THREADS) * 8;
+    float w[8];
+    load8<VEC>(a.pre, c, H, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * r * w[j];
+    if (a.h != nullptr) store8<VEC>(a.h + t * a.h_stride, c, H, v[i]);
+    if (a.codes != nullptr) {
+      const uint32_t amax = amax_half_warp(amax8(v[i]));
+      const uint2 q = codes8(v[i], block_inverse(amax));
+      uint8_t* const cr = a.codes + t * a.codes_stride;
+      if (VEC) {
+        if (c < H) *reinterpret_cast<uint2*>(cr + c) = q;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (c + j < H) cr[c + j] = (uint8_t)((j < 4 ? q.x : q.y) >> (8 * (j & 3)));
+      }
+      if ((threadIdx.x & 15) == 0 && c < H) a.scales[t * a.scales_stride + c / kScaleBlock] = block_scale(amax);
+    }
+  }
+}
+
+template <typename R, bool VEC>
+cudaError_t launch_norm_kind(cudaStream_t st, const NormArgs& a) {
+  const dim3 row((unsigned)a.tokens);
+  if (a.hidden <= 256) return launch_pdl(norm_kernel<R, 32, 1, VEC>, dim3((unsigned)((a.tokens + 3) / 4)), dim3(128), 0, st, a);
+  if (a.hidden <= 1024) return launch_pdl(norm_kernel<R, 128, 1, VEC>, row, dim3(128), 0, st, a);
+  if (a.hidden <= 2048) return launch_pdl(norm_kernel<R, 256, 1, VEC>, row, dim3(256), 0, st, a);
+  if (a.hidden <= 4096) return launch_pdl(norm_kernel<R, 256, 2, VEC>, row, dim3(256), 0, st, a);
+  if (a.hidden <= 8192) return launch_pdl(norm_kernel<R, 512, 2, VEC>, row, dim3(512), 0, st, a);
+  return launch_pdl(norm_kernel<R, 512, 4, VEC>, row, dim3(512), 0, st, a);
+}
+
+}  // namespace
+
+int norm_residual(const oled_norm_shape* shape, const void* x, const void* y, const void* post_weight, const void* gate,
+                  const void* pre_weight, int32_t n_tokens, cudaStream_t st, void* x_out, void* h, void* h_codes, float* h_scales) {
+  if (!shape) return OLED_ERR_INVALID_ARG;
+  const oled_norm_shape& s = *shape;
+  const int H = s.hidden, blocks = (H + kScaleBlock - 1) / kScaleBlock;
+  if (H <= 0 || H > 16384 || (s.residual != OLED_BF16 && s.residual != OLED_FP32) || s.gate_tokens < 0 || n_tokens < 0 ||
+      !(s.eps > 0.0f) || !std::isfinite(s.eps) || !std::isfinite(s.residual_scale))
+    return OLED_ERR_INVALID_ARG;
+  if (n_tokens == 0) return OLED_OK;
+  const int64_t item = s.residual == OLED_FP32 ? 4 : 2, T = n_tokens;
+  if (!x || (!y && (post_weight || gate)) || ((h || h_codes) != (pre_weight != nullptr)) || ((h_codes != nullptr) != (h_scales != nullptr)) ||
+      (!x_out && !h && !h_codes))
+    return OLED_ERR_INVALID_ARG;
+  if (s.x_stride < H || (y && s.y_stride < H) || (gate && s.gate_stride < H) || (x_out && s.x_out_stride < H) ||
+      (h && s.h_stride < H) || (h_codes && (s.codes_stride < H || s.scales_stride < blocks)))
+    return OLED_ERR_INVALID_ARG;
+  if (off_boundary(x, item) || off_boundary(x_out, item) || off_boundary(y, 2) || off_boundary(post_weight, 2) || off_boundary(gate, 2) ||
+      off_boundary(pre_weight, 2) || off_boundary(h, 2) || off_boundary(h_scales, 4))
+    return OLED_ERR_INVALID_ARG;
+  const int64_t gate_rows = s.gate_tokens > 0 ? (T + s.gate_tokens - 1) / s.gate_tokens : 1;
+  const RowRange in[] = {{x, s.x_stride * item, H * item, T},       {y, s.y_stride * 2, H * 2, T}, {post_weight, H * 2, H * 2, 1},
+                         {gate, s.gate_stride * 2, H * 2, gate_rows}, {pre_weight, H * 2, H * 2, 1}};
+  const RowRange out[] = {{x_out, s.x_out_stride * item, H * item, T}, {h, s.h_stride * 2, H * 2, T},
+                          {h_codes, s.codes_stride, H, T},             {h_scales, s.scales_stride * 4, blocks * 4, T}};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (rows_overlap(out[i], out[j])) return OLED_ERR_INVALID_ARG;
+    for (int j = 0; j < 5; ++j) {
+      // an element of x or y is read by the thread that writes the same element of x_out or h, before it does
+      if (out[i].p && (i == 0 || i == 1) && (j == 0 || j == 1) && same_rows(out[i], in[j])) continue;
+      if (rows_overlap(out[i], in[j])) return OLED_ERR_INVALID_ARG;
+    }
+  }
+  NormArgs a;
+  a.x = x;
+  a.y = static_cast<const uint16_t*>(y);
+  a.post = static_cast<const uint16_t*>(post_weight);
+  a.gate = static_cast<const uint16_t*>(gate);
+  a.pre = static_cast<const uint16_t*>(pre_weight);
+  a.x_out = x_out;
+  a.h = static_cast<uint16_t*>(h);
+  a.codes = static_cast<uint8_t*>(h_codes);
+  a.scales = h_scales;
+  a.x_stride = s.x_stride;
+  a.y_stride = s.y_stride;
+  a.gate_stride = s.gate_stride;
+  a.x_out_stride = s.x_out_stride;
+  a.h_stride = s.h_stride;
+  a.codes_stride = s.codes_stride;
+  a.scales_stride = s.scales_stride;
+  a.tokens = n_tokens;
+  a.hidden = H;
+  a.gate_tokens = s.gate_tokens;
+  a.eps = s.eps;
+  a.scale = s.residual_scale;
+  // 16-byte vectors where every row that is touched starts on a 16-byte boundary (codes: 8) and holds whole ones
+  bool vec = H % 8 == 0;
+  auto rows_ok = [&](const void* p, int64_t stride_bytes, uintptr_t align) {
+    if (p != nullptr) vec = vec && !off_boundary(p, align) && stride_bytes % (int64_t)align == 0;
+  };
+  rows_ok(x, s.x_stride * item, 16);
+  rows_ok(x_out, s.x_out_stride * item, 16);
+  rows_ok(y, s.y_stride * 2, 16);
+  rows_ok(gate, s.gate_stride * 2, 16);
+  rows_ok(post_weight, 0, 16);
+  rows_ok(pre_weight, 0, 16);
+  rows_ok(h, s.h_stride * 2, 16);
+  rows_ok(h_codes, s.codes_stride, 8);
+  cudaError_t err;
+  if (s.residual == OLED_FP32) err = vec ? launch_norm_kind<float, true>(st, a) : launch_norm_kind<float, false>(st, a);
+  else err = vec ? launch_norm_kind<uint16_t, true>(st, a) : launch_norm_kind<uint16_t, false>(st, a);
+  return cudaGetLastError() == cudaSuccess && err == cudaSuccess ? OLED_OK : OLED_ERR_CUDA;
+}
+
+}  // namespace oled
+
+extern "C" int oled_norm_residual(const oled_norm_shape* shape, const void* x, const void* y, const void* post_weight,
+                                  const void* gate, const void* pre_weight, int32_t n_tokens, void* cuda_stream, void* x_out,
+                                  void* h, void* h_codes, float* h_scales) {
+  return oled::norm_residual(shape, x, y, post_weight, gate, pre_weight, n_tokens, static_cast<cudaStream_t>(cuda_stream), x_out, h,
+                             h_codes, h_scales);
+}

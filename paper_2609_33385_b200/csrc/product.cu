@@ -1,0 +1,357 @@
+// C[m, n] = sum_k A[m, k] B[n, k] (+ D[m, n]) of e4m3 codes with block scales (oled_matmul_blocks): one fp32 scale per row
+// of A and 128 columns, one per 128 x 128 block of B.
+//
+// The scales change every 128 values of k, so a k-block's product is summed by the tensor cores alone (kind::f8f6f4, fp32 in
+// tensor memory) and then added, times its two scales, to fp32 accumulators in registers: C = sum_b (sa sb)_b (A_b B_b^T).
+// The scale of a row of A times that of the block of B is rounded once, the sums of k-blocks are fp32 fused multiply-adds.
+//
+// product_few_kernel: the weights are the MMA's M (128 rows, one block of scales), up to 128 rows of A its N, so that few
+// tokens cost few columns.  What bounds it is the weights' way into shared memory; where the tiles are fewer than the SMs, a cluster of
+// up to eight CTAs shares a tile's k-blocks and adds up through distributed shared memory, in the order of the k-blocks.
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include <algorithm>
+
+#include "block_scale.h"
+#include "kernels.h"
+#include "row_args.h"
+#include "sm100_ptx.h"
+
+namespace oled {
+namespace {
+
+struct ProductArgs {
+  const float* a_scale;
+  const float* b_scale;
+  const uint16_t* add;
+  void* out;
+  int64_t a_scale_stride, b_scale_stride, add_stride, out_stride;
+  int m, n, k_blocks, out_fp32;
+};
+
+__device__ __forceinline__ void store_result(const ProductArgs& p, int64_t row, int col, float v) {
+  if (p.add != nullptr) v += __uint_as_float((uint32_t)p.add[row * p.add_stride + col] << 16);
+  if (p.out_fp32) static_cast<float*>(p.out)[row * p.out_stride + col] = v;
+  else static_cast<uint16_t*>(p.out)[row * p.out_stride + col] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+}
+// Waits of these kernels are bounded like every other; there is no context to report to, so a tile whose wait ran out
+// becomes NaN.
+__device__ __forceinline__ bool product_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  unsigned long long t0 = 0;
+  for (uint32_t it = 0;; ++it) {
+    if (mbar_try(bar, parity)) return true;
+    if ((it & 1023u) == 1023u) {
+      if (*abort_flag) return false;
+      const unsigned long long now = globaltimer();
+      if (t0 == 0) t0 = now;
+      if (now - t0 > kWaitLimitNs) {
+        *abort_flag = 1;
+        return false;
+      }
+    }
+  }
+}
+__device__ __forceinline__ bool product_warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(0xffffffffu, product_wait(bar, parity, abort_flag)) != 0;
+}
+
+// ---- few rows of A ---------------------------------------------------------------------------
+constexpr int kFewStages = 8;   // at most
+constexpr int kFewAccs = 4;     // k-blocks whose products wait in tensor memory
+constexpr uint32_t kWTile = 128 * 128;
+__host__ __device__ constexpr int few_epi_warps(int nt) { return nt > 64 ? 8 : 4; }
+
+struct __align__(16) ProductFewCtl {
+  unsigned long long full[kFewStages];
+  unsigned long long empty[kFewStages];
+  unsigned long long acc_full[kFewAccs];
+  unsigned long long acc_empty[kFewAccs];
+  uint32_t tmem_base;
+  int abort;
+};
+
+// blockIdx.x: tile of 128 rows of B x the cluster's CTAs, blockIdx.y: tile of NT rows of A.  Dynamic shared memory: control,
+// [k-blocks of the CTA][NT] scales, then on a 1024-byte boundary the ring of `stages` (weight tile, rows of A), which
+// holds the CTA's [NT][128] partial sums in the end.
+template <int NT>
+__global__ void __launch_bounds__((few_epi_warps(NT) + 2) * 32, 1)
+product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a,
+                   const __grid_constant__ ProductArgs p, int stages, int split) {
+  constexpr int kEpi = few_epi_warps(NT), kProducer = kEpi, kMma = kEpi + 1;
+  constexpr int kCols = NT / (kEpi / 4);  // columns of an epilogue warp
+  constexpr uint32_t kStage = kWTile + NT * 128;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  ProductFewCtl* const ctl = reinterpret_cast<ProductFewCtl*>(smem_raw);
+  float* const s_scale = reinterpret_cast<float*>(smem_raw + sizeof(ProductFewCtl));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = split > 1 ? (int)cluster_cta_rank() : 0;
+  const int n_tile = (int)blockIdx.x / split, n0 = n_tile * 128, m0 = (int)blockIdx.y * NT;
+  const int kb0 = (int)((int64_t)p.k_blocks * rank / split), kb1 = (int)((int64_t)p.k_blocks * (rank + 1) / split);
+  const int kbs = kb1 - kb0;
+  const uint32_t ring = (smem_u32(s_scale) + (uint32_t)((p.k_blocks + split - 1) / split) * NT * 4u + 1023u) & ~1023u;
+  volatile int* const abort_flag = &ctl->abort;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) {
+      mbar_init(smem_u32(&ctl->full[s]), 1);
+      mbar_init(smem_u32(&ctl->empty[s]), 1);
+    }
+    for (int s = 0; s < kFewAccs; ++s) {
+      mbar_init(smem_u32(&ctl->acc_full[s]), 1);
+      mbar_init(smem_u32(&ctl->acc_empty[s]), kEpi);
+    }
+    ctl->abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == kProducer && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_b)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_a)) : "memory");
+  }
+  griddep_wait();
+  // Tensor memory is taken only once the kernel in front has given its own back, the kernel behind starts only once every
+  // CTA has its share, and nobody holds any while waiting for another CTA: no two can wait for each other's.
+  if (warp == kMma) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)),
+                 "r"(kFewAccs * NT)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  griddep_launch_dependents();
+  const uint32_t tmem = ctl->tmem_base;
+
+  float acc[kCols];
+  if (warp == kProducer) {
+    bool ok = true;
+    for (int i = 0; i < kbs && ok; ++i) {
+      const int stage = i % stages;
+      ok = product_warp_wait(smem_u32(&ctl->empty[stage]), ((uint32_t)(i / stages) & 1u) ^ 1u, abort_flag);
+      if (ok && elect_one()) {
+        const uint32_t bar = smem_u32(&ctl->full[stage]), dst = ring + (uint32_t)stage * kStage;
+        mbar_expect_tx(bar, kStage);
+        tma_load_2d(&map_b, dst, bar, (kb0 + i) * 128, n0);
+        tma_load_2d(&map_a, dst + kWTile, bar, (kb0 + i) * 128, m0);
+      }
+      __syncwarp();
+    }
+    if (!ok) {  // let copies already issued land before the CTA's shared memory is released
+      const unsigned long long t0 = globaltimer();
+      while (globaltimer() - t0 < 2000000ull) {
+      }
+    }
+  } else if (warp == kMma) {
+    const uint64_t w_desc0 = make_smem_desc(ring), x_desc0 = make_smem_desc(ring + kWTile);
+    const uint32_t idesc = make_idesc_e4m3(NT);
+    for (int i = 0; i < kbs; ++i) {
+      const int stage = i % stages, buf = i % kFewAccs;
+      if (!product_warp_wait(smem_u32(&ctl->acc_empty[buf]), ((uint32_t)(i / kFewAccs) & 1u) ^ 1u, abort_flag)) break;
+      if (!product_warp_wait(smem_u32(&ctl->full[stage]), (uint32_t)(i / stages) & 1u, abort_flag)) break;
+      tc_fence_after();
+      if (elect_one()) {
+        const uint64_t off = (uint64_t)((uint32_t)stage * (kStage >> 4));
+        const uint32_t d = tmem + (uint32_t)(buf * NT);
+        tc_mma_desc<true, false>(d, w_desc0 + off, x_desc0 + off, idesc);
+#pragma unroll
+        for (int k = 1; k < 4; ++k) tc_mma_desc<true, true>(d, w_desc0 + off + k * 2, x_desc0 + off + k * 2, idesc);
+        tc_commit(smem_u32(&ctl->empty[stage]));
+        tc_commit(smem_u32(&ctl->acc_full[buf]));
+      }
+      __syncwarp();
+    }
+  } else {
+    // scales of the CTA's k-blocks, those of A times that of B; zero behind the last row
+    for (int i = threadIdx.x; i < kbs * NT; i += kEpi * 32) {
+      const int c = i / kbs, b = i - c * kbs;
+      float s = 0.0f;
+      if (m0 + c < p.m)
+        s = p.a_scale[(int64_t)(m0 + c) * p.a_scale_stride + kb0 + b] * p.b_scale[(int64_t)n_tile * p.b_scale_stride + kb0 + b];
+      s_scale[b * NT + c] = s;
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(kEpi * 32) : "memory");
+    const int quarter = warp & 3, c0 = (warp >> 2) * kCols;
+    const uint32_t t_row = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c0;
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) acc[c] = 0.0f;
+    bool ok = true;
+    for (int i = 0; i < kbs && ok; ++i) {
+      const int buf = i % kFewAccs;
+      ok = product_warp_wait(smem_u32(&ctl->acc_full[buf]), (uint32_t)(i / kFewAccs) & 1u, abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+      constexpr int kPiece = kCols < 32 ? kCols : 32;
+#pragma unroll
+      for (int cc = 0; cc < kCols; cc += kPiece) {
+        uint32_t v[kPiece / 16][16];
+#pragma unroll
+        for (int q = 0; q < kPiece / 16; ++q) tmem_ld16(t_row + (uint32_t)(buf * NT + cc + q * 16), v[q]);
+        tmem_ld_wait();
+        if (cc + kPiece == kCols) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[buf]));
+        }
+        const float4* const sc = reinterpret_cast<const float4*>(s_scale + i * NT + c0 + cc);
+#pragma unroll
+        for (int q = 0; q < kPiece / 4; ++q) {
+          const float4 s = sc[q];
+          acc[cc + 4 * q] = fmaf(__uint_as_float(v[q / 4][(4 * q) % 16]), s.x, acc[cc + 4 * q]);
+          acc[cc + 4 * q + 1] = fmaf(__uint_as_float(v[q / 4][(4 * q + 1) % 16]), s.y, acc[cc + 4 * q + 1]);
+          acc[cc + 4 * q + 2] = fmaf(__uint_as_float(v[q / 4][(4 * q + 2) % 16]), s.z, acc[cc + 4 * q + 2]);
+          acc[cc + 4 * q + 3] = fmaf(__uint_as_float(v[q / 4][(4 * q + 3) % 16]), s.w, acc[cc + 4 * q + 3]);
+        }
+      }
+    }
+    if (!ok) {
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) acc[c] = __int_as_float(0x7fffffff);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMma) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kFewAccs * NT) : "memory");
+  }
+  const int row = (warp & 3) * 32 + lane, col0 = (warp >> 2) * kCols;
+  if (split == 1) {
+    if (warp < kEpi && n0 + row < p.n) {
+#pragma unroll
+      for (int c = 0; c < kCols; ++c)
+        if (m0 + col0 + c < p.m) store_result(p, m0 + col0 + c, n0 + row, acc[c]);
+    }
+    return;
+  }
+  // every CTA's partial sums in its own ring; CTA r adds up and stores its share of the columns
+  if (warp < kEpi) {
+#pragma unroll
+    for (int c = 0; c < kCols; ++c)
+      asm volatile("st.shared.f32 [%0], %1;" ::"r"(ring + (uint32_t)((col0 + c) * 128 + row) * 4u), "f"(acc[c]) : "memory");
+  }
+  cluster_sync_all();
+  if (warp < kEpi) {
+    const int c_end = min(NT / split * (rank + 1), p.m - m0);
+    for (int c = NT / split * rank + (warp >> 2); c < c_end; c += kEpi / 4) {
+      const uint32_t at = ring + (uint32_t)(c * 128 + row) * 4u;
+      float part[8];
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        if (s < split) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part[s]) : "r"(map_to_cta(at, (uint32_t)s)) : "memory");
+      float sum = part[0];
+#pragma unroll
+      for (int s = 1; s < 8; ++s)
+        if (s < split) sum += part[s];
+      if (n0 + row < p.n) store_result(p, m0 + c, n0 + row, sum);
+    }
+  }
+  cluster_sync_all();  // nobody leaves while another CTA may still read its sums
+}
+
+constexpr size_t kProductSmem = 222 * 1024;
+
+bool byte_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t stride, int box_rows) {
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride};
+  const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+  return encode_tensor_map(m, 2, base, dims, strides, box, true);
+}
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, int cluster, Args&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  attr[n].id = cudaLaunchAttributeClusterDimension;
+  attr[n].val.clusterDim.x = (unsigned)cluster;
+  attr[n].val.clusterDim.y = 1;
+  attr[n++].val.clusterDim.z = 1;
+  if (pdl_enabled()) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+template <int NT>
+int launch_few(cudaStream_t st, const CUtensorMap& map_b, const CUtensorMap& map_a, const ProductArgs& p) {
+  // (per device: the attribute belongs to the kernel of the current context)
+  if (cudaFuncSetAttribute(product_few_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kProductSmem) != cudaSuccess)
+    return OLED_ERR_CUDA;
+  const int tiles_n = (p.n + 127) / 128, tiles_m = (p.m + NT - 1) / NT;
+  int split = 1;
+  while (split < 8 && 2 * split <= p.k_blocks && (int64_t)tiles_n * tiles_m * split * 2 <= 148) split *= 2;
+  const int kbs = (p.k_blocks + split - 1) / split;
+  constexpr size_t kStage = kWTile + NT * 128;
+  const size_t fixed = sizeof(ProductFewCtl) + (size_t)kbs * NT * 4 + 2048;
+  const int stages = (int)std::min<size_t>({(size_t)kFewStages, (size_t)kbs, (kProductSmem - fixed) / kStage});
+  const size_t smem = fixed + std::max(stages * kStage, split > 1 ? (size_t)NT * 512 : 0);
+  const cudaError_t err = launch_cluster(product_few_kernel<NT>, dim3((unsigned)(tiles_n * split), (unsigned)tiles_m),
+                                         dim3((few_epi_warps(NT) + 2) * 32), smem, st, split, map_b, map_a, p, stages, split);
+  return err == cudaSuccess ? OLED_OK : OLED_ERR_CUDA;
+}
+
+}  // namespace
+
+int matmul_blocks(const oled_product_shape* shape, const void* a, const float* a_scale, const void* b, const float* b_scale,
+                     const void* add, int32_t m, cudaStream_t st, void* out) {
+  if (!shape) return OLED_ERR_INVALID_ARG;
+  const oled_product_shape& s = *shape;
+  if (s.n <= 0 || s.n > (1 << 20) || s.k <= 0 || s.k > OLED_MAX_PRODUCT_K || s.k % 16 != 0 || (s.out != OLED_BF16 && s.out != OLED_FP32) || m < 0)
+    return OLED_ERR_INVALID_ARG;
+  const int kb = (s.k + 127) / 128, nb = (s.n + 127) / 128;
+  if (s.a_stride < s.k || s.a_stride % 16 != 0 || s.b_stride < s.k || s.b_stride % 16 != 0 || s.a_scale_stride < kb || s.b_scale_stride < kb ||
+      s.out_stride < s.n || (add && s.add_stride < s.n) || s.a_stride >= (1ll << 40) || s.b_stride >= (1ll << 40))
+    return OLED_ERR_INVALID_ARG;
+  if (m > OLED_MAX_ROUTE_TOKENS) return OLED_ERR_TOO_MANY_TOKENS;
+  if (m == 0) return OLED_OK;
+  const int64_t item = s.out == OLED_FP32 ? 4 : 2;
+  if (!a || !a_scale || !b || !b_scale || !out || off_boundary(a, 16) || off_boundary(b, 16) || off_boundary(a_scale, 4) ||
+      off_boundary(b_scale, 4) || off_boundary(add, 2) || off_boundary(out, item))
+    return OLED_ERR_INVALID_ARG;
+  {
+    const RowRange o{out, s.out_stride * item, s.n * item, m}, d{add, s.add_stride * 2, (int64_t)s.n * 2, m};
+    const RowRange in[] = {{a, s.a_stride, s.k, m}, {a_scale, s.a_scale_stride * 4, kb * 4, m}, {b, s.b_stride, s.k, s.n}, {b_scale, s.b_scale_stride * 4, kb * 4, nb}};
+    for (const RowRange& r : in)
+      if (rows_overlap(o, r)) return OLED_ERR_INVALID_ARG;
+    if (!same_rows(o, d) && rows_overlap(o, d)) return OLED_ERR_INVALID_ARG;  // (in place: an element is read before it is written)
+  }
+  ProductArgs p;
+  p.a_scale = a_scale;
+  p.b_scale = b_scale;
+  p.add = static_cast<const uint16_t*>(add);
+  p.out = out;
+  p.a_scale_stride = s.a_scale_stride;
+  p.b_scale_stride = s.b_scale_stride;
+  p.add_stride = s.add_stride;
+  p.out_stride = s.out_stride;
+  p.m = m;
+  p.n = s.n;
+  p.k_blocks = kb;
+  p.out_fp32 = s.out == OLED_FP32;
+  const int nt = m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128;
+  CUtensorMap map_a, map_b;
+  if (!byte_map(&map_a, a, m, s.k, s.a_stride, nt) || !byte_map(&map_b, b, s.n, s.k, s.b_stride, 128)) return OLED_ERR_CUDA;
+  int rc;
+  switch (nt) {
+    case 16: rc = launch_few<16>(st, map_b, map_a, p); break;
+    case 32: rc = launch_few<32>(st, map_b, map_a, p); break;
+    case 64: rc = launch_few<64>(st, map_b, map_a, p); break;
+    default: rc = launch_few<128>(st, map_b, map_a, p); break;
+  }
+  return cudaGetLastError() == cudaSuccess ? rc : OLED_ERR_CUDA;
+}
+
+}  // namespace oled
+
+extern "C" int oled_matmul_blocks(const oled_product_shape* shape, const void* a, const float* a_scale, const void* b,
+                                     const float* b_scale, const void* add, int32_t m, void* cuda_stream, void* out) {
+  return oled::matmul_blocks(shape, a, a_scale, b, b_scale, add, m, static_cast<cudaStream_t>(cuda_stream), out);
+}
