@@ -693,7 +693,7 @@ EncodeTiledFn get_encode_fn() {
 
 }  // namespace
 bool encode_tensor_map(CUtensorMap* m, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
-                       const cuuint32_t* box, bool bytes, bool narrow) {
+                       const cuuint32_t* box, bool bytes, bool narrow, bool words) {
   EncodeTiledFn fn = get_encode_fn();
   if (!fn) return false;
   cuuint32_t estr[5] = {1, 1, 1, 1, 1};
@@ -702,7 +702,7 @@ bool encode_tensor_map(CUtensorMap* m, int rank, const void* base, const cuuint6
   // widening form (64 bytes per k-block) land with the 64-byte swizzle, which lets 32 lanes read
   // 32 rows free of bank conflicts; e4m3 rows the MMA reads itself (128 bytes per k-block) land
   // in the 128-byte-swizzled layout again
-  return fn(m, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank,
+  return fn(m, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : words ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank,
             const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             narrow ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, promo,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

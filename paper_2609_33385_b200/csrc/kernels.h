@@ -311,9 +311,9 @@ int launch_ffn_pair(cudaStream_t st, const FfnTcMaps& maps, const FfnGroup& grp,
 constexpr int kFfnWorkCounters = 8;  // FFN launches of one layer execution: 3 groups x 2 kinds, rounded up
 constexpr int kFfnCounterWords = 2;  // words of each launch's work counter
 
-// A tensor map over bf16 elements (bytes: over bytes) with the 128-byte swizzle (narrow: the 64-byte one).
+// A tensor map over bf16 elements (bytes: over bytes; words: over fp32) with the 128-byte swizzle (narrow: the 64-byte one).
 bool encode_tensor_map(CUtensorMap* m, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
-                       const cuuint32_t* box, bool bytes = false, bool narrow = false);
+                       const cuuint32_t* box, bool bytes = false, bool narrow = false, bool words = false);
 // ---- ffn_few.cu: token tiles of at most kFewMaxRows rows (bf16 stores, or fp8 stores with the token
 // terms at hand).  Kinds as above; kind 2 of fp8 stores is preceded by the split kernel.
 constexpr int kFewMaxRows = 128;  // the largest token tile of ffn_few.cu

@@ -8,6 +8,12 @@
 // product_few_kernel: the weights are the MMA's M (128 rows, one block of scales), up to 128 rows of A its N, so that few
 // tokens cost few columns.  What bounds it is the weights' way into shared memory; where the tiles are fewer than the SMs, a cluster of
 // up to eight CTAs shares a tile's k-blocks and adds up through distributed shared memory, in the order of the k-blocks.
+//
+// product_pair_kernel: many rows.  A pair of CTAs computes 256 rows of A x 256 of B with M = 256 MMAs (cta_group::2): each CTA
+// holds 128 rows of A and of the accumulators and half of the rows of B, 32 KB a k-block for 512 cycles of MMAs (one CTA alone
+// on 128 x 256 would need 48 KB, more than an SM's share of L2 delivers in that time).  Here the rows of A are
+// the accumulators' lanes, so that a thread's scale is one number per k-block.  Eight warps read a k-block's 128 x 256 products
+// from tensor memory (two buffers) and add them to 128 registers a thread beside the next k-block's MMAs; results leave through shared memory as bulk tensor stores where rows of C are on 16-byte boundaries.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -37,23 +43,18 @@ __device__ __forceinline__ void store_result(const ProductArgs& p, int64_t row, 
 }
 // Waits of these kernels are bounded like every other; there is no context to report to, so a tile whose wait ran out
 // becomes NaN.
-__device__ __forceinline__ bool product_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+// (The warp stays converged: polling lane by lane cost 100 cycles more where the barrier was ready.)
+__device__ __forceinline__ bool product_warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   unsigned long long t0 = 0;
-  for (uint32_t it = 0;; ++it) {
-    if (mbar_try(bar, parity)) return true;
-    if ((it & 1023u) == 1023u) {
-      if (*abort_flag) return false;
+  for (uint32_t it = 1; !__all_sync(0xffffffffu, mbar_try(bar, parity)); ++it) {
+    if ((it & 1023u) == 0u) {
       const unsigned long long now = globaltimer();
       if (t0 == 0) t0 = now;
-      if (now - t0 > kWaitLimitNs) {
-        *abort_flag = 1;
-        return false;
-      }
+      if (now - t0 > kWaitLimitNs) *abort_flag = 1;
+      if (__any_sync(0xffffffffu, *abort_flag != 0)) return false;
     }
   }
-}
-__device__ __forceinline__ bool product_warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  return __all_sync(0xffffffffu, product_wait(bar, parity, abort_flag)) != 0;
+  return true;
 }
 
 // ---- few rows of A ---------------------------------------------------------------------------
@@ -250,12 +251,261 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
   cluster_sync_all();  // nobody leaves while another CTA may still read its sums
 }
 
+// ---- many rows of A: pairs of CTAs -------------------------------------------------------------
+constexpr int kManyEpiWarps = 8, kManyProducer = 8, kManyMma = 9, kManyThreads = 12 * 32;
+// Registers a thread: 168 at launch (12 warps), of which the third warpgroup gives to the two that accumulate: 4 x 56 + 8 x 224 = 12 x 168.
+constexpr int kManyFewRegs = 56, kManyEpiRegs = 224;
+constexpr int kManyStages = 5, kManyRows = 256, kManyCols = 256;  // of a pair's tile
+constexpr uint32_t kManyStage = 2 * kWTile;
+constexpr uint32_t kManyOut = 8192;  // staging of a warp's results: 32 rows x 128 bytes, twice
+
+struct __align__(16) ProductManyCtl {
+  unsigned long long full[kManyStages];   // in the first CTA: both CTAs' copies
+  unsigned long long empty[kManyStages];  // in both
+  unsigned long long acc_full[2];         // in both
+  unsigned long long acc_empty[2];        // in the first CTA: the epilogue warps of both
+  uint32_t tmem_base;
+  int abort;
+};
+constexpr uint32_t kManySmem = 1024 + kManyStages * kManyStage + kManyEpiWarps * kManyOut + 1024;
+static_assert(sizeof(ProductManyCtl) <= 1024, "control block");
+
+// The pair's tiles are dealt out in turn (tile t of pair t mod pairs), rows of A first: the pairs of a moment share rows of B.
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kManyThreads, 1)
+product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a,
+                    const __grid_constant__ CUtensorMap map_out, const __grid_constant__ ProductArgs p, int bulk_out) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  ProductManyCtl* const ctl = reinterpret_cast<ProductManyCtl*>(smem_raw);
+  const uint32_t ring = (smem_u32(smem_raw) + sizeof(ProductManyCtl) + 1023u) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_cta_rank();
+  const int pair = (int)blockIdx.x >> 1, n_pairs = (int)gridDim.x >> 1;
+  const int tiles_m = (p.m + kManyRows - 1) / kManyRows, tiles = tiles_m * ((p.n + kManyCols - 1) / kManyCols);
+  const int kbs = p.k_blocks;
+  volatile int* const abort_flag = &ctl->abort;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kManyStages; ++s) {
+      mbar_init(smem_u32(&ctl->full[s]), 1);
+      mbar_init(smem_u32(&ctl->empty[s]), 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(smem_u32(&ctl->acc_full[s]), 1);
+      mbar_init(smem_u32(&ctl->acc_empty[s]), 2 * kManyEpiWarps);
+    }
+    ctl->abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == kManyProducer && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_b)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_a)) : "memory");
+  }
+  griddep_wait();
+  if (warp == kManyMma) {  // (all of it: no other kernel that takes tensor memory fits beside this one's shared memory)
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  griddep_launch_dependents();
+  const uint32_t tmem = ctl->tmem_base;
+  const uint32_t full_on_first = map_to_cta(smem_u32(&ctl->full[0]), 0), acc_empty_on_first = map_to_cta(smem_u32(&ctl->acc_empty[0]), 0);
+
+  if (warp >= kManyEpiWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kManyFewRegs));
+  if (warp == kManyProducer) {
+    bool ok = true;
+    int stage = 0;
+    uint32_t phase = 0;
+    for (int tile = pair; tile < tiles && ok; tile += n_pairs) {
+      const int row_a = (tile % tiles_m) * kManyRows + (int)rank * 128, row_b = (tile / tiles_m) * kManyCols + (int)rank * 128;
+      for (int kb = 0; kb < kbs; ++kb) {
+        ok = product_warp_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, abort_flag);
+        if (!ok) break;
+        if (elect_one()) {
+          const uint32_t bar = full_on_first + (uint32_t)stage * 8u, dst = ring + (uint32_t)stage * kManyStage;
+          if (rank == 0) mbar_expect_tx(smem_u32(&ctl->full[stage]), 2 * kManyStage);
+          tma_load_2d_pair(&map_a, dst, bar, kb * 128, row_a);
+          tma_load_2d_pair(&map_b, dst + kWTile, bar, kb * 128, row_b);
+        }
+        __syncwarp();
+        if (++stage == kManyStages) {
+          stage = 0;
+          phase ^= 1u;
+        }
+      }
+    }
+    if (!ok) {  // let copies already issued land before the CTA's shared memory is released
+      const unsigned long long t0 = globaltimer();
+      while (globaltimer() - t0 < 2000000ull) {
+      }
+    }
+  } else if (warp == kManyMma && rank == 0) {
+    const uint64_t a_desc0 = make_smem_desc(ring), b_desc0 = make_smem_desc(ring + kWTile);
+    const uint32_t idesc = make_idesc_pair_e4m3(kManyCols);
+    bool ok = true;
+    int stage = 0, buf = 0;
+    uint32_t phase = 0, acc_phase = 0;
+    for (int tile = pair; tile < tiles && ok; tile += n_pairs)
+      for (int kb = 0; kb < kbs; ++kb) {
+        ok = product_warp_wait(smem_u32(&ctl->full[stage]), phase, abort_flag) &&
+             product_warp_wait(smem_u32(&ctl->acc_empty[buf]), acc_phase ^ 1u, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t off = (uint64_t)((uint32_t)stage * (kManyStage >> 4));
+          const uint32_t d = tmem + (uint32_t)(buf * kManyCols);
+          tc_mma_pair_e4m3<false>(d, a_desc0 + off, b_desc0 + off, idesc);
+#pragma unroll
+          for (int k = 1; k < 4; ++k) tc_mma_pair_e4m3<true>(d, a_desc0 + off + k * 2, b_desc0 + off + k * 2, idesc);
+          tc_commit_pair(smem_u32(&ctl->acc_full[buf]), 3u);
+          tc_commit_pair(smem_u32(&ctl->empty[stage]), 3u);
+        }
+        __syncwarp();
+        if (++stage == kManyStages) {
+          stage = 0;
+          phase ^= 1u;
+        }
+        buf ^= 1;
+        if (buf == 0) acc_phase ^= 1u;
+      }
+  }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyEpiRegs));
+    // warp w: lane quarter w mod 4, the block of 128 columns w / 4
+    const int quarter = warp & 3, half = warp >> 2;
+    const uint32_t t_row = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
+    const uint32_t stage_out = ring + kManyStages * kManyStage + (uint32_t)warp * kManyOut;
+    bool ok = true;
+    int buf = 0;
+    uint32_t acc_phase = 0;
+    for (int tile = pair; tile < tiles; tile += n_pairs) {
+      const int row = (tile % tiles_m) * kManyRows + (int)rank * 128 + quarter * 32 + lane;
+      const int col0 = (tile / tiles_m) * kManyCols + half * 128;
+      const float* const sa = p.a_scale + (int64_t)min(row, p.m - 1) * p.a_scale_stride;
+      const float* const sb = p.b_scale + (int64_t)(min(col0, p.n - 1) / 128) * p.b_scale_stride;
+      float acc[128];
+#pragma unroll
+      for (int c = 0; c < 128; ++c) acc[c] = 0.0f;
+      // scales, fetched two k-blocks ahead (the shared memory leaves little L1: they come from L2)
+      float s_a = __ldg(sa), s_b = __ldg(sb), next_a = __ldg(sa + min(1, kbs - 1)), next_b = __ldg(sb + min(1, kbs - 1));
+      for (int kb = 0; kb < kbs && ok; ++kb) {
+        const float s = s_a * s_b;
+        s_a = next_a;
+        s_b = next_b;
+        next_a = __ldg(sa + min(kb + 2, kbs - 1));
+        next_b = __ldg(sb + min(kb + 2, kbs - 1));
+        ok = product_warp_wait(smem_u32(&ctl->acc_full[buf]), acc_phase, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          uint32_t v[64];
+          tmem_ld64(t_row + (uint32_t)(buf * kManyCols + q * 64), v);
+          tmem_ld_wait();
+          if (q == 1) {  // the buffer is handed back before its last columns are added
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty_on_first + (uint32_t)buf * 8u);
+          }
+#pragma unroll
+          for (int c = 0; c < 64; ++c) acc[q * 64 + c] = fmaf(__uint_as_float(v[c]), s, acc[q * 64 + c]);
+        }
+        buf ^= 1;
+        if (buf == 0) acc_phase ^= 1u;
+      }
+      if (!ok) {
+#pragma unroll
+        for (int c = 0; c < 128; ++c) acc[c] = __int_as_float(0x7fffffff);
+      }
+      if (p.add != nullptr && row < p.m) {
+        const uint16_t* const d = p.add + (int64_t)row * p.add_stride + col0;
+#pragma unroll
+        for (int c = 0; c < 128; ++c)
+          if (col0 + c < p.n) acc[c] += __uint_as_float((uint32_t)d[c] << 16);
+      }
+      if (bulk_out) {
+        // rows of 128 bytes, 16-byte pieces where the 128-byte swizzle wants them; a piece of 64 bf16 or 32 fp32 columns at a time
+        const int row0 = row - lane;
+#pragma unroll
+        for (int round = 0; round < 2; ++round) {  // of two pieces, the staging's two halves
+          if (round == 1 && !p.out_fp32) break;
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the stores before have been read
+          __syncwarp();
+#pragma unroll
+          for (int piece = 0; piece < 2; ++piece) {
+            const uint32_t line = stage_out + (uint32_t)piece * 4096u + (uint32_t)lane * 128u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              uint32_t w[4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                if (p.out_fp32) {
+                  w[q] = __float_as_uint(acc[(round * 2 + piece) * 32 + j * 4 + q]);
+                } else {
+                  const __nv_bfloat162 h = __floats2bfloat162_rn(acc[piece * 64 + j * 8 + 2 * q], acc[piece * 64 + j * 8 + 2 * q + 1]);
+                  w[q] = *reinterpret_cast<const uint32_t*>(&h);
+                }
+              }
+              asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(line + (uint32_t)((j ^ (lane & 7)) * 16)), "r"(w[0]), "r"(w[1]),
+                           "r"(w[2]), "r"(w[3])
+                           : "memory");
+            }
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0 && row0 < p.m) {  // (rows and columns behind the end are left as they are)
+#pragma unroll
+            for (int piece = 0; piece < 2; ++piece) {
+              const int col = col0 + (p.out_fp32 ? (round * 2 + piece) * 32 : piece * 64);
+              if (col < p.n)
+                asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(&map_out),
+                             "r"(stage_out + (uint32_t)piece * 4096u), "r"(col), "r"(row0)
+                             : "memory");
+            }
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          }
+        }
+      } else if (row < p.m) {
+#pragma unroll
+        for (int c = 0; c < 128; ++c)
+          if (col0 + c < p.n) {
+            if (p.out_fp32) static_cast<float*>(p.out)[(int64_t)row * p.out_stride + col0 + c] = acc[c];
+            else static_cast<uint16_t*>(p.out)[(int64_t)row * p.out_stride + col0 + c] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[c]));
+          }
+      }
+    }
+    if (bulk_out && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+  // nobody leaves while the partner may still read this CTA's shared memory or arrive on its barriers
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  if (warp == kManyMma) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
 constexpr size_t kProductSmem = 222 * 1024;
+constexpr int kFewRows = 512;
 
 bool byte_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t stride, int box_rows) {
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride};
   const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
   return encode_tensor_map(m, 2, base, dims, strides, box, true);
+}
+
+// C in pieces of 32 rows x 128 bytes
+bool output_map(CUtensorMap* m, const ProductArgs& p) {
+  const cuuint64_t item = p.out_fp32 ? 4 : 2;
+  const cuuint64_t dims[2] = {(cuuint64_t)p.n, (cuuint64_t)p.m}, strides[1] = {(cuuint64_t)p.out_stride * item};
+  const cuuint32_t box[2] = {(cuuint32_t)(128 / item), 32};
+  return encode_tensor_map(m, 2, p.out, dims, strides, box, false, false, p.out_fp32);
 }
 
 template <typename... KArgs, typename... Args>
@@ -298,6 +548,20 @@ int launch_few(cudaStream_t st, const CUtensorMap& map_b, const CUtensorMap& map
   return err == cudaSuccess ? OLED_OK : OLED_ERR_CUDA;
 }
 
+int launch_pair(cudaStream_t st, const CUtensorMap& map_b, const CUtensorMap& map_a, const ProductArgs& p) {
+  if (cudaFuncSetAttribute(product_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kManySmem) != cudaSuccess)
+    return OLED_ERR_CUDA;
+  const int64_t item = p.out_fp32 ? 4 : 2;
+  CUtensorMap map_out = map_a;
+  const bool bulk = !off_boundary(p.out, 16) && p.out_stride * item % 16 == 0 && p.out_stride * item < (1ll << 40);
+  if (bulk && !output_map(&map_out, p)) return OLED_ERR_CUDA;
+  const int tiles = (p.m + kManyRows - 1) / kManyRows * ((p.n + kManyCols - 1) / kManyCols);
+  const int pairs = std::min(tiles, 148 / 2);
+  const cudaError_t err = launch_pdl(product_pair_kernel, dim3((unsigned)(2 * pairs)), dim3(kManyThreads), kManySmem, st, map_b, map_a, map_out, p,
+                                     bulk ? 1 : 0);
+  return err == cudaSuccess ? OLED_OK : OLED_ERR_CUDA;
+}
+
 }  // namespace
 
 int matmul_blocks(const oled_product_shape* shape, const void* a, const float* a_scale, const void* b, const float* b_scale,
@@ -336,8 +600,13 @@ int matmul_blocks(const oled_product_shape* shape, const void* a, const float* a
   p.n = s.n;
   p.k_blocks = kb;
   p.out_fp32 = s.out == OLED_FP32;
-  const int nt = m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128;
   CUtensorMap map_a, map_b;
+  if (m > kFewRows) {
+    if (!byte_map(&map_a, a, m, s.k, s.a_stride, 128) || !byte_map(&map_b, b, s.n, s.k, s.b_stride, 128)) return OLED_ERR_CUDA;
+    const int rc = launch_pair(st, map_b, map_a, p);
+    return cudaGetLastError() == cudaSuccess ? rc : OLED_ERR_CUDA;
+  }
+  const int nt = m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128;
   if (!byte_map(&map_a, a, m, s.k, s.a_stride, nt) || !byte_map(&map_b, b, s.n, s.k, s.b_stride, 128)) return OLED_ERR_CUDA;
   int rc;
   switch (nt) {
