@@ -33,13 +33,36 @@ struct ProductArgs {
   const uint16_t* add;
   void* out;
   int64_t a_scale_stride, b_scale_stride, add_stride, out_stride;
-  int m, n, k_blocks, out_fp32;
+  int m, n, k_blocks, out_fp32, vec;  // vec: see store_four
 };
 
-__device__ __forceinline__ void store_result(const ProductArgs& p, int64_t row, int col, float v) {
-  if (p.add != nullptr) v += __uint_as_float((uint32_t)p.add[row * p.add_stride + col] << 16);
-  if (p.out_fp32) static_cast<float*>(p.out)[row * p.out_stride + col] = v;
-  else static_cast<uint16_t*>(p.out)[row * p.out_stride + col] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+// Four consecutive columns of a row of C.  vec: rows of C (and of D) start on boundaries of four elements.
+__device__ __forceinline__ void store_four(const ProductArgs& p, int64_t row, int col, float (&v)[4], bool vec) {
+  const uint16_t* const d = p.add != nullptr ? p.add + row * p.add_stride + col : nullptr;
+  if (vec && col + 3 < p.n) {
+    if (d != nullptr) {
+      const uint2 w = *reinterpret_cast<const uint2*>(d);
+      v[0] += __uint_as_float(w.x << 16);
+      v[1] += __uint_as_float(w.x & 0xffff0000u);
+      v[2] += __uint_as_float(w.y << 16);
+      v[3] += __uint_as_float(w.y & 0xffff0000u);
+    }
+    if (p.out_fp32) {
+      *reinterpret_cast<float4*>(static_cast<float*>(p.out) + row * p.out_stride + col) = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+      const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + row * p.out_stride + col) =
+          make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (col + j < p.n) {
+      const float r = d != nullptr ? v[j] + __uint_as_float((uint32_t)d[j] << 16) : v[j];
+      if (p.out_fp32) static_cast<float*>(p.out)[row * p.out_stride + col + j] = r;
+      else static_cast<uint16_t*>(p.out)[row * p.out_stride + col + j] = __bfloat16_as_ushort(__float2bfloat16_rn(r));
+    }
 }
 // Waits of these kernels are bounded like every other; there is no context to report to, so a tile whose wait ran out
 // becomes NaN.
@@ -72,6 +95,43 @@ struct __align__(16) ProductFewCtl {
   int abort;
 };
 
+// Sums of the SPLIT CTAs' partial results ([NT][128] at `ring` in each), and their stores: CTA `rank` has NT / SPLIT columns, a
+// warp one at a time, UNROLL of them requested together (one after the other a column took 170 ns).
+template <int NT, int SPLIT, int UNROLL>
+__device__ __forceinline__ void join_columns(const ProductArgs& p, uint32_t ring, int rank, int warp, int lane, int m0, int n0) {
+  constexpr int kShare = NT / SPLIT, kEpi = few_epi_warps(NT);
+  const int c_end = min(kShare * (rank + 1), p.m - m0);
+  uint32_t base[SPLIT];
+#pragma unroll
+  for (int s = 0; s < SPLIT; ++s) base[s] = map_to_cta(ring + (uint32_t)lane * 16u, (uint32_t)s);
+#pragma unroll 1
+  for (int c = kShare * rank + warp; c < c_end; c += kEpi * UNROLL) {
+    float4 part[UNROLL][SPLIT];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      const uint32_t at = (uint32_t)min(c + u * kEpi, NT - 1) * 512u;
+#pragma unroll
+      for (int s = 0; s < SPLIT; ++s)  // (no memory clobber: the loads need not wait for the stores of other columns)
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(part[u][s].x), "=f"(part[u][s].y), "=f"(part[u][s].z), "=f"(part[u][s].w)
+                     : "r"(base[s] + at));
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      if (c + u * kEpi >= c_end) break;
+      float v[4] = {part[u][0].x, part[u][0].y, part[u][0].z, part[u][0].w};
+#pragma unroll
+      for (int s = 1; s < SPLIT; ++s) {
+        v[0] += part[u][s].x;
+        v[1] += part[u][s].y;
+        v[2] += part[u][s].z;
+        v[3] += part[u][s].w;
+      }
+      store_four(p, m0 + c + u * kEpi, n0 + lane * 4, v, p.vec != 0);
+    }
+  }
+}
+
 // blockIdx.x: tile of 128 rows of B x the cluster's CTAs, blockIdx.y: tile of NT rows of A.  Dynamic shared memory: control,
 // [k-blocks of the CTA][NT] scales, then on a 1024-byte boundary the ring of `stages` (weight tile, rows of A), which
 // holds the CTA's [NT][128] partial sums in the end.
@@ -92,32 +152,51 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
   const int kbs = kb1 - kb0;
   const uint32_t ring = (smem_u32(s_scale) + (uint32_t)((p.k_blocks + split - 1) / split) * NT * 4u + 1023u) & ~1023u;
   volatile int* const abort_flag = &ctl->abort;
+  const auto load = [&](int i, int stage) {
+    const uint32_t bar = smem_u32(&ctl->full[stage]), dst = ring + (uint32_t)stage * kStage;
+    mbar_expect_tx(bar, kStage);
+    tma_load_2d(&map_b, dst, bar, (kb0 + i) * 128, n0);
+    tma_load_2d(&map_a, dst + kWTile, bar, (kb0 + i) * 128, m0);
+  };
 
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < stages; ++s) {
-      mbar_init(smem_u32(&ctl->full[s]), 1);
-      mbar_init(smem_u32(&ctl->empty[s]), 1);
+  // Before the CTA's first barrier: the first loads are on their way, tensor memory is taken, the scales are in place.
+  if (warp == kProducer) {
+    if (lane == 0) {
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_b)) : "memory");
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_a)) : "memory");
+      for (int s = 0; s < stages; ++s) {
+        mbar_init(smem_u32(&ctl->full[s]), 1);
+        mbar_init(smem_u32(&ctl->empty[s]), 1);
+      }
+      for (int s = 0; s < kFewAccs; ++s) {
+        mbar_init(smem_u32(&ctl->acc_full[s]), 1);
+        mbar_init(smem_u32(&ctl->acc_empty[s]), kEpi);
+      }
+      ctl->abort = 0;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      griddep_wait();
+      for (int i = 0; i < min(stages, kbs); ++i) load(i, i);
     }
-    for (int s = 0; s < kFewAccs; ++s) {
-      mbar_init(smem_u32(&ctl->acc_full[s]), 1);
-      mbar_init(smem_u32(&ctl->acc_empty[s]), kEpi);
-    }
-    ctl->abort = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
-  if (warp == kProducer && lane == 0) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_b)) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_a)) : "memory");
-  }
-  griddep_wait();
-  // Tensor memory is taken only once the kernel in front has given its own back, the kernel behind starts only once every
-  // CTA has its share, and nobody holds any while waiting for another CTA: no two can wait for each other's.
-  if (warp == kMma) {
+    __syncwarp();
+  } else if (warp == kMma) {
+    // Tensor memory is taken only once the kernel in front has given its own back, the kernel behind starts only once every
+    // CTA has its share, and nobody holds any while waiting for another CTA: no two can wait for each other's.
+    griddep_wait();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)),
                  "r"(kFewAccs * NT)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  } else {
+    // scales of the CTA's k-blocks, those of A times that of B; zero behind the last row
+    griddep_wait();
+    for (int i = threadIdx.x; i < kbs * NT; i += kEpi * 32) {
+      const int c = i / kbs, b = i - c * kbs;
+      float s = 0.0f;
+      if (m0 + c < p.m)
+        s = p.a_scale[(int64_t)(m0 + c) * p.a_scale_stride + kb0 + b] * p.b_scale[(int64_t)n_tile * p.b_scale_stride + kb0 + b];
+      s_scale[b * NT + c] = s;
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -128,15 +207,10 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
   float acc[kCols];
   if (warp == kProducer) {
     bool ok = true;
-    for (int i = 0; i < kbs && ok; ++i) {
+    for (int i = stages; i < kbs && ok; ++i) {
       const int stage = i % stages;
       ok = product_warp_wait(smem_u32(&ctl->empty[stage]), ((uint32_t)(i / stages) & 1u) ^ 1u, abort_flag);
-      if (ok && elect_one()) {
-        const uint32_t bar = smem_u32(&ctl->full[stage]), dst = ring + (uint32_t)stage * kStage;
-        mbar_expect_tx(bar, kStage);
-        tma_load_2d(&map_b, dst, bar, (kb0 + i) * 128, n0);
-        tma_load_2d(&map_a, dst + kWTile, bar, (kb0 + i) * 128, m0);
-      }
+      if (ok && elect_one()) load(i, stage);
       __syncwarp();
     }
     if (!ok) {  // let copies already issued land before the CTA's shared memory is released
@@ -164,15 +238,6 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
       __syncwarp();
     }
   } else {
-    // scales of the CTA's k-blocks, those of A times that of B; zero behind the last row
-    for (int i = threadIdx.x; i < kbs * NT; i += kEpi * 32) {
-      const int c = i / kbs, b = i - c * kbs;
-      float s = 0.0f;
-      if (m0 + c < p.m)
-        s = p.a_scale[(int64_t)(m0 + c) * p.a_scale_stride + kb0 + b] * p.b_scale[(int64_t)n_tile * p.b_scale_stride + kb0 + b];
-      s_scale[b * NT + c] = s;
-    }
-    asm volatile("bar.sync 1, %0;" ::"n"(kEpi * 32) : "memory");
     const int quarter = warp & 3, c0 = (warp >> 2) * kCols;
     const uint32_t t_row = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c0;
 #pragma unroll
@@ -212,43 +277,27 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
     }
   }
   tc_fence_before();
-  __syncthreads();
+  __syncthreads();  // the MMAs have read the ring
   if (warp == kMma) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kFewAccs * NT) : "memory");
   }
-  const int row = (warp & 3) * 32 + lane, col0 = (warp >> 2) * kCols;
-  if (split == 1) {
-    if (warp < kEpi && n0 + row < p.n) {
-#pragma unroll
-      for (int c = 0; c < kCols; ++c)
-        if (m0 + col0 + c < p.m) store_result(p, m0 + col0 + c, n0 + row, acc[c]);
-    }
-    return;
-  }
-  // every CTA's partial sums in its own ring; CTA r adds up and stores its share of the columns
+  // Every CTA's partial sums go to its own ring; CTA r adds up and stores its share of the columns, a warp one column at a time.
+  // (Stored by the lanes that hold them, 64 columns of two bytes each took longer than the product itself.)
   if (warp < kEpi) {
+    const uint32_t at = ring + (uint32_t)((warp >> 2) * kCols * 128 + (warp & 3) * 32 + lane) * 4u;
 #pragma unroll
-    for (int c = 0; c < kCols; ++c)
-      asm volatile("st.shared.f32 [%0], %1;" ::"r"(ring + (uint32_t)((col0 + c) * 128 + row) * 4u), "f"(acc[c]) : "memory");
+    for (int c = 0; c < kCols; ++c) asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + (uint32_t)c * 512u), "f"(acc[c]) : "memory");
   }
-  cluster_sync_all();
+  if (split > 1) cluster_sync_all();
+  else __syncthreads();
   if (warp < kEpi) {
-    const int c_end = min(NT / split * (rank + 1), p.m - m0);
-    for (int c = NT / split * rank + (warp >> 2); c < c_end; c += kEpi / 4) {
-      const uint32_t at = ring + (uint32_t)(c * 128 + row) * 4u;
-      float part[8];
-#pragma unroll
-      for (int s = 0; s < 8; ++s)
-        if (s < split) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part[s]) : "r"(map_to_cta(at, (uint32_t)s)) : "memory");
-      float sum = part[0];
-#pragma unroll
-      for (int s = 1; s < 8; ++s)
-        if (s < split) sum += part[s];
-      if (n0 + row < p.n) store_result(p, m0 + c, n0 + row, sum);
-    }
+    if (split == 1) join_columns<NT, 1, 4>(p, ring, 0, warp, lane, m0, n0);
+    else if (split == 2) join_columns<NT, 2, 4>(p, ring, rank, warp, lane, m0, n0);
+    else if (split == 4) join_columns<NT, 4, 2>(p, ring, rank, warp, lane, m0, n0);
+    else join_columns<NT, 8, 2>(p, ring, rank, warp, lane, m0, n0);
   }
-  cluster_sync_all();  // nobody leaves while another CTA may still read its sums
+  if (split > 1) cluster_sync_all();  // nobody leaves while another CTA may still read its sums
 }
 
 // ---- many rows of A: pairs of CTAs -------------------------------------------------------------
@@ -492,7 +541,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
 }
 
 constexpr size_t kProductSmem = 222 * 1024;
-constexpr int kFewRows = 512;
+constexpr int kFewRows = 256;
 
 bool byte_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t stride, int box_rows) {
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride};
@@ -542,7 +591,7 @@ int launch_few(cudaStream_t st, const CUtensorMap& map_b, const CUtensorMap& map
   constexpr size_t kStage = kWTile + NT * 128;
   const size_t fixed = sizeof(ProductFewCtl) + (size_t)kbs * NT * 4 + 2048;
   const int stages = (int)std::min<size_t>({(size_t)kFewStages, (size_t)kbs, (kProductSmem - fixed) / kStage});
-  const size_t smem = fixed + std::max(stages * kStage, split > 1 ? (size_t)NT * 512 : 0);
+  const size_t smem = fixed + std::max(stages * kStage, (size_t)NT * 512);
   const cudaError_t err = launch_cluster(product_few_kernel<NT>, dim3((unsigned)(tiles_n * split), (unsigned)tiles_m),
                                          dim3((few_epi_warps(NT) + 2) * 32), smem, st, split, map_b, map_a, p, stages, split);
   return err == cudaSuccess ? OLED_OK : OLED_ERR_CUDA;
@@ -600,6 +649,7 @@ int matmul_blocks(const oled_product_shape* shape, const void* a, const float* a
   p.n = s.n;
   p.k_blocks = kb;
   p.out_fp32 = s.out == OLED_FP32;
+  p.vec = !off_boundary(out, 4 * item) && s.out_stride % 4 == 0 && (!add || (!off_boundary(add, 8) && s.add_stride % 4 == 0));
   CUtensorMap map_a, map_b;
   if (m > kFewRows) {
     if (!byte_map(&map_a, a, m, s.k, s.a_stride, 128) || !byte_map(&map_b, b, s.n, s.k, s.b_stride, 128)) return OLED_ERR_CUDA;
