@@ -557,28 +557,6 @@ bool output_map(CUtensorMap* m, const ProductArgs& p) {
   return encode_tensor_map(m, 2, p.out, dims, strides, box, false, false, p.out_fp32);
 }
 
-template <typename... KArgs, typename... Args>
-cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, int cluster, Args&&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  int n = 0;
-  attr[n].id = cudaLaunchAttributeClusterDimension;
-  attr[n].val.clusterDim.x = (unsigned)cluster;
-  attr[n].val.clusterDim.y = 1;
-  attr[n++].val.clusterDim.z = 1;
-  if (pdl_enabled()) {
-    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[n++].val.programmaticStreamSerializationAllowed = 1;
-  }
-  cfg.attrs = attr;
-  cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
-}
-
 template <int NT>
 int launch_few(cudaStream_t st, const CUtensorMap& map_b, const CUtensorMap& map_a, const ProductArgs& p) {
   // (per device: the attribute belongs to the kernel of the current context)

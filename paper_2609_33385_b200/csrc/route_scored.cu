@@ -16,18 +16,20 @@
 // consecutive, so that lower lanes hold lower experts and a group never shares a lane with another.  Every lane
 // sorts its keys once (a network of maxima and minima in registers); then each of the top_k rounds is one warp maximum
 // over the lanes' heads, a vote for the lowest lane that has it, and a shift in that lane.
-// Bound by the instructions of a token (some 250 at 256 experts top-8; the logits' bytes would take a third of the time).
+// Bound by the instructions of a token; the logits' bytes would take a third of the time.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "kernels.h"
 #include "route_math.h"
 #include "row_args.h"
+#include "sm100_ptx.h"
 
 namespace oled {
 namespace {
 
-constexpr int kScoredWarps = 8;
+constexpr int kScoredWarps = 16;
 constexpr int kScoredThreads = kScoredWarps * 32;
 
 struct ScoredArgs {
@@ -38,7 +40,7 @@ struct ScoredArgs {
   float* gate;
   int T, E, K, G, top_groups, group_top, softmax, renormalise;
   float scale;
-  int group_size, lanes_per_group, per_lane, vec;
+  int group_size, lanes_per_group, lanes_log2, per_lane, vec;
   // tokens of CTA c: segment c / parts, of seg_tokens tokens, and there the part c % parts, of part_tokens
   int parts, seg_tokens, part_tokens;
   // (nullptr: not wanted) per expert and CTA, [E][n_ctas]
@@ -64,9 +66,6 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 __device__ __forceinline__ float no_nan(float v) { return v == v ? v : __int_as_float(0xff800000); }
-// exp(l - top): one for the largest logit even where it is infinite
-__device__ __forceinline__ float softmax_term(float l, float top) { return l == top ? 1.0f : __expf(l - top); }
-
 // Descending order of N keys in registers.
 template <int N>
 __device__ __forceinline__ void sort_desc(uint32_t (&k)[N]) {
@@ -86,101 +85,123 @@ __device__ __forceinline__ void sort_desc(uint32_t (&k)[N]) {
       }
 }
 
-// The choice of one token in fp64, by a warp: lane r < K ends with the id of rank r.  Experts e = lane + 32 i.  (Loops that
-// are not unrolled keep the arrays in local memory: the registers of this rare path count for the whole kernel.)
-__device__ __noinline__ int select_exact(const ScoredArgs& a, const float* row, int lane) {
-  constexpr int kPer = OLED_MAX_EXPERTS / 32;
+__device__ __forceinline__ unsigned long long order_key64(double v) {  // v is not NaN and not -0
+  const unsigned long long bits = (unsigned long long)__double_as_longlong(v);
+  return (bits >> 63) ? ~bits : (bits | 0x8000000000000000ull);
+}
+
+// exp(x) in fp64 for |x| <= 708 (clamped beyond), without a branch so that several run side by side: x = n ln 2 + r with ln 2 in two
+// parts (Cody and Waite), the Taylor polynomial of degree 13 for |r| <= ln 2 / 2 (its remainder is below 2^-57 of the
+// result), and n added to the exponent.  Off by a few units in the last place.
+__device__ __forceinline__ double exp_double(double x) {
+  x = fmin(fmax(x, -708.0), 708.0);
+  const double n = rint(x * 1.4426950408889634074);
+  double r = fma(-n, 6.93147180369123816490e-01, x);  // ln 2 without its low 21 bits: n times it is exact
+  r = fma(-n, 1.90821492927058770002e-10, r);
+  double p = 1.0 / 6227020800.0;
+  p = fma(p, r, 1.0 / 479001600.0);
+  p = fma(p, r, 1.0 / 39916800.0);
+  p = fma(p, r, 1.0 / 3628800.0);
+  p = fma(p, r, 1.0 / 362880.0);
+  p = fma(p, r, 1.0 / 40320.0);
+  p = fma(p, r, 1.0 / 5040.0);
+  p = fma(p, r, 1.0 / 720.0);
+  p = fma(p, r, 1.0 / 120.0);
+  p = fma(p, r, 1.0 / 24.0);
+  p = fma(p, r, 1.0 / 6.0);
+  p = fma(p, r, 0.5);
+  p = fma(p, r, 1.0);
+  p = fma(p, r, 1.0);
+  return __longlong_as_double(__double_as_longlong(p) + ((long long)(int)n << 52));
+}
+// 1 / x for normal x, by Newton's iteration from an approximation of 2^-20.
+__device__ __forceinline__ double reciprocal_double(double x) {
+  double y;
+  asm("rcp.approx.ftz.f64 %0, %1;" : "=d"(y) : "d"(x));
+  y = fma(y, fma(-x, y, 1.0), y);
+  y = fma(y, fma(-x, y, 1.0), y);
+  return y;
+}
+
+// The choice of one token in fp64, by the warp that holds its logits: lane r < K ends with the id of rank r.  Scores below
+// exp(-708) count as that.  Few tokens come here, but a CTA waits for the last of its own: four experts of a lane side by side (with
+// exp() and quotients one after the other a token took 5.5 us).  The arrays lie in local memory, since registers count for the whole kernel.
+template <int PER>
+__device__ __noinline__ int select_exact(const ScoredArgs& a, const float* row, int lane, int first, int mine, float top) {
+  constexpr int kSide = PER < 4 ? PER : 4;
   const double kNone = -INFINITY;
-  double score[kPer], choice[kPer];
-  double top = kNone;
-#pragma unroll 1
-  for (int i = 0; i < kPer; ++i) {
-    const int e = lane + 32 * i;
-    score[i] = e < a.E ? (double)no_nan(row[e]) : kNone;
-    top = fmax(top, score[i]);
+  double value[PER];             // exponentials
+  unsigned long long key[PER];   // of the choices, 0: not to be had
+  float logit[PER], bias[PER];   // (all of them requested at once)
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    logit[i] = i < mine ? row[first + i] : 0.0f;
+    bias[i] = i < mine && a.bias != nullptr ? a.bias[first + i] : 0.0f;
   }
-  for (int d = 16; d >= 1; d >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, d));
   double sum = 0.0;
 #pragma unroll 1
-  for (int i = 0; i < kPer; ++i) {
-    const int e = lane + 32 * i;
-    if (e >= a.E) continue;
-    const double l = score[i];
-    score[i] = a.softmax ? (l == top ? 1.0 : exp(l - top)) : 1.0 / (1.0 + exp(-l));
-    sum += score[i];
-    choice[i] = a.bias != nullptr ? 0.0 : l;
-  }
-  for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-  uint32_t allowed = 0xffffffffu;  // groups
-#pragma unroll 1
-  for (int i = 0; i < kPer; ++i) {
-    const int e = lane + 32 * i;
-    if (e >= a.E) continue;
-    if (a.softmax) score[i] /= sum;
-    if (a.bias != nullptr) {
-      const double c = score[i] + (double)a.bias[e];
-      choice[i] = row[e] == row[e] && c == c ? c : kNone;
-      score[i] = choice[i];
+  for (int i0 = 0; i0 < mine; i0 += kSide)
+#pragma unroll
+    for (int i = i0; i < i0 + kSide; ++i) {
+      const float l = no_nan(logit[i]);
+      const double e = exp_double(a.softmax ? (l == top ? 0.0 : (double)l - (double)top) : -(double)l);
+      value[i] = e;
+      if (i < mine) sum += e;
     }
-  }
-  if (a.G > 1 && a.top_groups < a.G) {
-    double mine = kNone;  // the value of group `lane`
+  for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  double t1 = kNone, t2 = kNone;
 #pragma unroll 1
-    for (int g = 0; g < a.G; ++g) {
-      double t1 = kNone, t2 = kNone;
-#pragma unroll 1
-      for (int i = 0; i < kPer; ++i) {
-        const int e = lane + 32 * i;
-        if (e < g * a.group_size || e >= (g + 1) * a.group_size) continue;
-        const double v = a.group_top == 1 ? choice[i] : score[i];
+  for (int i0 = 0; i0 < mine; i0 += kSide)
+#pragma unroll
+    for (int i = i0; i < i0 + kSide; ++i) {
+      const float l = logit[i];
+      const double score = (a.softmax ? value[i] : 1.0) * reciprocal_double(a.softmax ? sum : 1.0 + value[i]);
+      double c = a.bias == nullptr ? (double)l : score + (double)bias[i];
+      if (!(l == l) || !(c == c)) c = kNone;
+      key[i] = order_key64(c + 0.0);
+      if (i < mine) {
+        const double v = a.bias != nullptr || a.group_top == 1 ? c : score;
         t2 = fmax(t2, fmin(t1, v));
         t1 = fmax(t1, v);
       }
-      for (int d = 16; d >= 1; d >>= 1) {
-        const double o1 = __shfl_xor_sync(0xffffffffu, t1, d), o2 = __shfl_xor_sync(0xffffffffu, t2, d);
-        t2 = fmax(fmin(t1, o1), fmax(t2, o2));
-        t1 = fmax(t1, o1);
-      }
-      double v = a.group_top == 1 ? t1 : t1 + t2;
-      if (!(v == v)) v = kNone;
-      if (lane == g) mine = v;
     }
+  if (a.G > 1) {
+#pragma unroll 1
+    for (int d = a.lanes_per_group >> 1; d >= 1; d >>= 1) {
+      const double o1 = __shfl_xor_sync(0xffffffffu, t1, d), o2 = __shfl_xor_sync(0xffffffffu, t2, d);
+      t2 = fmax(fmin(t1, o1), fmax(t2, o2));
+      t1 = fmax(t1, o1);
+    }
+    double v = a.group_top == 1 ? t1 : t1 + t2;
+    if (!(v == v)) v = kNone;
+    const int g = lane >> a.lanes_log2;
     int before = 0;
 #pragma unroll 1
-    for (int g = 0; g < a.G; ++g) {
-      const double v = __shfl_sync(0xffffffffu, mine, g);
-      before += v > mine || (v == mine && g < lane);
+    for (int o = 0; o < a.G; ++o) {
+      const double w = __shfl_sync(0xffffffffu, v, o << a.lanes_log2);
+      before += w > v || (w == v && o < g);
     }
-    allowed = __ballot_sync(0xffffffffu, lane < a.G && before < a.top_groups);
-  }
-  uint32_t left = 0u;
-#pragma unroll 1
-  for (int i = 0; i < kPer; ++i) {
-    const int e = lane + 32 * i;
-    if (e < a.E && ((allowed >> (e / a.group_size)) & 1u)) left |= 1u << i;
+    if (before >= a.top_groups) mine = 0;
   }
   int id = 0;
 #pragma unroll 1
   for (int r = 0; r < a.K; ++r) {
-    double bv = 0.0;
-    int be = 0x7fffffff;
+    unsigned long long best = 0ull;
+    int at = 0;
 #pragma unroll 1
-    for (int i = 0; i < kPer; ++i)
-      if ((left >> i) & 1u)
-        if (be == 0x7fffffff || choice[i] > bv) {
-          bv = choice[i];
-          be = lane + 32 * i;
+    for (int i0 = 0; i0 < mine; i0 += kSide)
+#pragma unroll
+      for (int i = i0; i < i0 + kSide; ++i)
+        if (i < mine && key[i] > best) {  // (ascending i: the lower index stays)
+          best = key[i];
+          at = i;
         }
-    for (int d = 16; d >= 1; d >>= 1) {
-      const double ov = __shfl_xor_sync(0xffffffffu, bv, d);
-      const int oe = __shfl_xor_sync(0xffffffffu, be, d);
-      if (oe != 0x7fffffff && (be == 0x7fffffff || ov > bv || (ov == bv && oe < be))) {
-        bv = ov;
-        be = oe;
-      }
-    }
-    if ((be & 31) == lane) left &= ~(1u << (be >> 5));
-    if (lane == r) id = be;
+    const uint32_t hi = (uint32_t)(best >> 32), hi_max = __reduce_max_sync(0xffffffffu, hi);
+    const uint32_t lo = hi == hi_max ? (uint32_t)best : 0u, lo_max = __reduce_max_sync(0xffffffffu, lo);
+    const int winner = __ffs((int)__ballot_sync(0xffffffffu, hi == hi_max && (uint32_t)best == lo_max)) - 1;
+    const int chosen = __shfl_sync(0xffffffffu, first + at, winner);
+    if (lane == winner) key[at] = 0ull;
+    if (lane == r) id = chosen;
   }
   return id;
 }
@@ -193,139 +214,179 @@ __device__ __forceinline__ bool near_choices(float a, float b, float slack) {
   return !(a - b > slack + 2.4e-7f * fmaxf(fabsf(a), fabsf(b)));
 }
 
-// PER: experts a lane has room for.
-template <int PER>
-__device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane, const float (&bias)[PER], int first, int mine,
-                                            int32_t* s_counts, unsigned long long* s_scores) {
-  const float* const row = a.logits + (int64_t)t * a.stride;
-  float l[PER];
-  if (a.vec) {
+// The fp32 forms the choice starts from.  exp2 and the reciprocal are off by 2^-22 and 2^-23 of their results.
+__device__ __forceinline__ float fast_exp(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.4426950408889634f));
+  return r;
+}
+__device__ __forceinline__ float fast_reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float fast_sigmoid(float l) { return fast_reciprocal(1.0f + fast_exp(-l)); }
+// order_key() in two instructions; a NaN's is above that of +inf or below that of -inf.
+__device__ __forceinline__ uint32_t sort_key(float v) {
+  const uint32_t bits = __float_as_uint(v);
+  return bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u);
+}
+
+// A token's logits, as its lanes hold them.  PER: experts a lane has room for.  FULL: every lane has that many.
+template <int PER, bool FULL>
+__device__ __forceinline__ void load_logits(const ScoredArgs& a, int t, int first, int mine, float (&l)[PER]) {
+  const float* const row = a.logits + (int64_t)t * a.stride + first;
+  if (PER >= 4 && a.vec) {
 #pragma unroll
-    for (int i = 0; i < PER; i += 4)
-      if (PER >= 4 && i < mine) {
-        const float4 v = *reinterpret_cast<const float4*>(row + first + i);
+    for (int i = 0; i + 3 < PER; i += 4)
+      if (FULL || i < mine) {
+        const float4 v = *reinterpret_cast<const float4*>(row + i);
         l[i] = v.x;
-        if (i + 1 < PER) l[i + 1] = v.y;
-        if (i + 2 < PER) l[i + 2] = v.z;
-        if (i + 3 < PER) l[i + 3] = v.w;
+        l[i + 1] = v.y;
+        l[i + 2] = v.z;
+        l[i + 3] = v.w;
       }
   } else {
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-      if (i < mine) l[i] = row[first + i];
+      if (FULL || i < mine) l[i] = row[i];
   }
+}
+
+template <int PER, bool FULL>
+__device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane, const float (&l)[PER], const float (&bias)[PER], int first,
+                                            int mine_, int32_t* s_ids, int32_t* s_counts, unsigned long long* s_scores) {
+  const int mine = FULL ? PER : mine_;
+  const float* const row = a.logits + (int64_t)t * a.stride;
   const float kNone = __int_as_float(0xff800000);
-  float top = kNone, sum = 1.0f;
-  uint32_t nan = 0u;
+  float top = kNone, sum = 1.0f, slack = 0.0f;
+  bool near = false;  // decided again in fp64: near choices, and tokens with a NaN
+  uint32_t key[PER];
+  float z[PER];
+  if (a.softmax) {  // (fmaxf reads a NaN as -inf)
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    if (i >= mine) l[i] = kNone;
-    if (!(l[i] == l[i])) {
-      nan |= 1u << i;
-      l[i] = kNone;
-    }
-  }
-  float c[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) c[i] = l[i];
-  if (a.softmax) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) top = fmaxf(top, l[i]);
+    for (int i = 0; i < PER; ++i)
+      if (FULL || i < mine) top = fmaxf(top, l[i]);
     top = warp_max(top);
     sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const float z = i < mine ? softmax_term(l[i], top) : 0.0f;
-      sum += z;
-      if (a.bias != nullptr) c[i] = z;
+      const float x = fmaxf(l[i], kNone);
+      z[i] = FULL || i < mine ? (x == top ? 1.0f : fast_exp(x - top)) : 0.0f;
+      sum += z[i];
     }
     sum = warp_sum(sum);
   }
-  const float inverse = __fdividef(1.0f, sum);
-  float slack = 0.0f;
-  bool near = false;
+  const float inverse = fast_reciprocal(sum);
   if (a.bias != nullptr) {
     slack = a.softmax ? 9.2e-6f * inverse : 5.8e-7f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const float s = a.softmax ? c[i] * inverse : __fdividef(1.0f, 1.0f + __expf(-l[i]));
-      c[i] = (nan >> i) & 1u ? kNone : no_nan(s + bias[i]);
+      const float c = (a.softmax ? z[i] * inverse : fast_sigmoid(l[i])) + bias[i];
+      near = near || ((FULL || i < mine) && !(c + l[i] == c + l[i]));
+      key[i] = FULL || i < mine ? sort_key(c) : 0u;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      near = near || ((FULL || i < mine) && !(l[i] == l[i]));
+      key[i] = FULL || i < mine ? sort_key(__fadd_rn(l[i], 0.0f)) : 0u;  // (-0 as +0)
     }
   }
-  uint32_t key[PER], sorted[PER];
+  uint32_t sorted[PER];
 #pragma unroll
-  for (int i = 0; i < PER; ++i) key[i] = i < mine ? order_key(__fadd_rn(c[i], 0.0f)) : 0u;  // (-0 as +0)
-  if (a.G > 1 && a.top_groups < a.G) {
-    float t1 = kNone, t2 = kNone;
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (i < mine) {
-        t2 = fmaxf(t2, fminf(t1, c[i]));
-        t1 = fmaxf(t1, c[i]);
-      }
+  for (int i = 0; i < PER; ++i) sorted[i] = key[i];
+  sort_desc<PER>(sorted);
+  if (a.G > 1) {
+    // the two largest choices of the lane, then of its group
+    float t1 = sorted[0] != 0u ? key_value(sorted[0]) : kNone, t2 = PER > 1 && sorted[PER > 1 ? 1 : 0] != 0u ? key_value(sorted[PER > 1 ? 1 : 0]) : kNone;
     for (int d = a.lanes_per_group >> 1; d >= 1; d >>= 1) {
       const float o1 = __shfl_xor_sync(0xffffffffu, t1, d), o2 = __shfl_xor_sync(0xffffffffu, t2, d);
       t2 = fmaxf(fminf(t1, o1), fmaxf(t2, o2));
       t1 = fmaxf(t1, o1);
     }
-    float value = t1, group_slack = slack;
-    const bool exact = a.bias == nullptr && a.group_top == 1;
+    float group_slack = slack;
     if (a.group_top == 2) {
       if (a.bias == nullptr) {  // the order of scores is that of logits
         if (a.softmax) {
-          t1 = softmax_term(t1, top) * inverse;
-          t2 = softmax_term(t2, top) * inverse;
+          t1 = t1 == top ? inverse : fast_exp(t1 - top) * inverse;
+          t2 = t2 == top ? inverse : fast_exp(t2 - top) * inverse;
           group_slack = 9.2e-6f * inverse;
         } else {
-          t1 = __fdividef(1.0f, 1.0f + __expf(-t1));
-          t2 = __fdividef(1.0f, 1.0f + __expf(-t2));
+          t1 = fast_sigmoid(t1);
+          t2 = fast_sigmoid(t2);
           group_slack = 5.8e-7f;
         }
       }
-      value = no_nan(t1 + t2);
+      t1 += t2;
       group_slack *= 2.0f;
     }
-    const int g = lane / a.lanes_per_group;
+    const int g = lane >> a.lanes_log2;
+    const uint32_t value = order_key(topk_value(t1));
     int before = 0;
+#pragma unroll 4
     for (int o = 0; o < a.G; ++o) {
-      const float v = __shfl_sync(0xffffffffu, value, o * a.lanes_per_group);
-      before += v > value || (v == value && o < g);
-      if (!exact && o != g && g < a.G) near = near || near_choices(fmaxf(v, value), fminf(v, value), group_slack);
+      const uint32_t v = __shfl_sync(0xffffffffu, value, o << a.lanes_log2);
+      before += v > value - (o < g ? 1u : 0u);  // (an equal value precedes if its group is lower; no key is zero)
     }
-    if (before >= a.top_groups) {
+    const bool keep = before < a.top_groups;
+    if (a.bias != nullptr || a.group_top == 2) {  // the border between the groups that stay and the others
+      const uint32_t worst = __reduce_min_sync(0xffffffffu, keep && g < a.G ? value : 0xffffffffu);
+      const uint32_t best = __reduce_max_sync(0xffffffffu, !keep && g < a.G ? value : 0u);
+      near = near || near_choices(key_value(worst), key_value(best), group_slack);
+    }
+    if (!keep) {
 #pragma unroll
-      for (int i = 0; i < PER; ++i) key[i] = 0u;
+      for (int i = 0; i < PER; ++i) key[i] = sorted[i] = 0u;
     }
   }
-#pragma unroll
-  for (int i = 0; i < PER; ++i) sorted[i] = key[i];
-  sort_desc<PER>(sorted);
-  uint32_t my_key = 0u, next = 0u;
-  int my_lane = 0;
+  // Rounds: lane r ends with the r-th largest key and the lanes that had it at their head.  Every lane that has the largest
+  // key drops it, which is one lane unless keys are equal.
+  uint32_t my_key = 0u, my_lanes = 0u;
   for (int r = 0; r < a.K; ++r) {
     const uint32_t best = __reduce_max_sync(0xffffffffu, sorted[0]);
-    const int winner = __ffs((int)__ballot_sync(0xffffffffu, sorted[0] == best)) - 1;
+    const bool mine_is_best = sorted[0] == best;
+    const uint32_t lanes = __ballot_sync(0xffffffffu, mine_is_best);
     if (lane == r) {
       my_key = best;
-      my_lane = winner;
+      my_lanes = lanes;
     }
-    if (lane == winner) {
 #pragma unroll
-      for (int i = 0; i + 1 < PER; ++i) sorted[i] = sorted[i + 1];
-      sorted[PER - 1] = 0u;
-    }
+    for (int i = 0; i + 1 < PER; ++i) sorted[i] = mine_is_best ? sorted[i + 1] : sorted[i];
+    sorted[PER - 1] = mine_is_best ? 0u : sorted[PER - 1];
   }
-  next = __reduce_max_sync(0xffffffffu, sorted[0]);
-  {
+  if (a.bias != nullptr) {
     uint32_t after = __shfl_down_sync(0xffffffffu, my_key, 1);
+    const uint32_t next = __reduce_max_sync(0xffffffffu, sorted[0]);
     if (lane == a.K - 1) after = next;
-    if (a.bias != nullptr && lane < a.K && after != 0u) near = near || near_choices(key_value(my_key), key_value(after), slack);
+    if (lane < a.K && after != 0u) near = near || near_choices(key_value(my_key), key_value(after), slack);
+  }
+  near = __any_sync(0xffffffffu, near);
+  if (!near && __any_sync(0xffffffffu, lane < a.K && (my_lanes & (my_lanes - 1u)) != 0u)) {
+    // equal logits in several lanes (logits that were bf16 have them often): again, the lowest lane alone drops its key
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sorted[i] = key[i];
+    sort_desc<PER>(sorted);
+    for (int r = 0; r < a.K; ++r) {
+      const uint32_t best = __reduce_max_sync(0xffffffffu, sorted[0]);
+      const uint32_t lanes = __ballot_sync(0xffffffffu, sorted[0] == best), lowest = lanes & (0u - lanes);
+      if (lane == r) {
+        my_key = best;
+        my_lanes = lowest;
+      }
+      if ((lowest >> lane) & 1u) {
+#pragma unroll
+        for (int i = 0; i + 1 < PER; ++i) sorted[i] = sorted[i + 1];
+        sorted[PER - 1] = 0u;
+      }
+    }
   }
   int id;
-  if (__any_sync(0xffffffffu, near)) {
-    id = select_exact(a, row, lane);
+  if (near) {
+    id = select_exact<PER>(a, row, lane, first, mine, top);
   } else {
     // equal keys of one lane are taken in the order of their indices
+    const int my_lane = __ffs((int)my_lanes) - 1;
     int skip = 0;
     {
       const uint32_t before = __shfl_up_sync(0xffffffffu, my_key, 1);
@@ -337,35 +398,62 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
     int at = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const uint32_t k = __shfl_sync(0xffffffffu, key[i], my_lane);
+      const uint32_t k = __shfl_sync(0xffffffffu, key[i], my_lane & 31);
       if (k == my_key) {
         if (skip == 0) at = i;
         --skip;
       }
     }
-    id = __shfl_sync(0xffffffffu, first, my_lane) + at;
+    id = __shfl_sync(0xffffffffu, first, my_lane & 31) + at;
   }
-  // the chosen experts' weights
+  // the chosen experts' weights (the quotients are off by two units in the last place at most)
   float s = 0.0f;
   if (lane < a.K) {
     const float x = no_nan(row[id]);
-    s = a.softmax ? (x == top ? 1.0f : expf(x - top)) : __fdiv_rn(1.0f, 1.0f + expf(-x));
+    s = a.softmax ? (x == top ? 1.0f : expf(x - top)) : __fdividef(1.0f, 1.0f + expf(-x));
   }
   float w = s;
-  if (a.renormalise) w = __fdiv_rn(s, warp_sum(s) + 1e-20f * sum);  // (softmax: s is sum times the score)
-  else if (a.softmax) w = __fdiv_rn(s, sum);
+  if (a.renormalise) w = __fdividef(s, warp_sum(s) + 1e-20f * sum);  // (softmax: s is sum times the score)
+  else if (a.softmax) w = __fdividef(s, sum);
   if (lane < a.K) {
     a.ids[(int64_t)t * a.K + lane] = id;
     a.gate[(int64_t)t * a.K + lane] = w * a.scale;
+    if (s_ids != nullptr) s_ids[lane] = id;
     if (s_counts != nullptr) atomicAdd(&s_counts[id], 1);
     // (the numerators take the weight before its scale, at most one: their sums are reported in 48 bits)
     if (s_scores != nullptr) atomicAdd(&s_scores[id], score_quantum(w, a.conf[t]));
   }
 }
 
-// Dynamic shared memory: [E] scores (where wanted), [E] counts (where wanted).
+// The tokens begin + warp, begin + warp + kScoredWarps, ... of a CTA; the next one's logits are on their way while one is routed.
+template <int PER, bool FULL>
+__device__ __forceinline__ void route_tokens(const ScoredArgs& a, int begin, int end, int warp, int lane, const float (&bias)[PER], int first,
+                                             int mine, int32_t* s_ids, int32_t* s_counts, unsigned long long* s_scores) {
+  float l[PER];
+  int t = begin + warp;
+  if (t < end) load_logits<PER, FULL>(a, t, first, mine, l);
+  for (; t < end; t += kScoredWarps) {
+    float now[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) now[i] = l[i];
+    if (t + kScoredWarps < end) load_logits<PER, FULL>(a, t + kScoredWarps, first, mine, l);
+    route_token<PER, FULL>(a, t, lane, now, bias, first, mine, s_ids != nullptr ? s_ids + (t - begin) * a.K : nullptr, s_counts, s_scores);
+  }
+}
+
+// The experts of a lane, and their biases.
 template <int PER>
-__global__ void __launch_bounds__(kScoredThreads)
+__device__ __forceinline__ void lane_experts(const ScoredArgs& a, int lane, int& first, int& mine, float (&bias)[PER]) {
+  const int g = lane >> a.lanes_log2, sub = lane - (g << a.lanes_log2);
+  first = g < a.G ? g * a.group_size + sub * a.per_lane : 0;
+  mine = g < a.G ? max(0, min(a.per_lane, a.group_size - sub * a.per_lane)) : 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) bias[i] = a.bias != nullptr && i < mine ? a.bias[first + i] : 0.0f;
+}
+
+// Dynamic shared memory: [E] scores (where wanted), [E] counts (where wanted).
+template <int PER, bool FULL>
+__global__ void __launch_bounds__(kScoredThreads, PER <= 8 ? 2 : 1)
 route_scored_kernel(const __grid_constant__ ScoredArgs a) {
   extern __shared__ __align__(16) uint8_t s_dyn[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -381,16 +469,13 @@ route_scored_kernel(const __grid_constant__ ScoredArgs a) {
     __syncthreads();
   }
   griddep_wait();
-  const int g = lane / a.lanes_per_group, sub = lane - g * a.lanes_per_group;
-  const int first = g < a.G ? g * a.group_size + sub * a.per_lane : 0;
-  const int mine = g < a.G ? max(0, min(a.per_lane, a.group_size - sub * a.per_lane)) : 0;
+  int first, mine;
   float bias[PER];
-#pragma unroll
-  for (int i = 0; i < PER; ++i) bias[i] = a.bias != nullptr && i < mine ? a.bias[first + i] : 0.0f;
+  lane_experts<PER>(a, lane, first, mine, bias);
   const int seg = (int)blockIdx.x / a.parts, part = (int)blockIdx.x - seg * a.parts;
   const int begin = seg * a.seg_tokens + part * a.part_tokens;
   const int end = min(min(begin + a.part_tokens, (seg + 1) * a.seg_tokens), a.T);
-  for (int t = begin + warp; t < end; t += kScoredWarps) route_token<PER>(a, t, lane, bias, first, mine, s_counts, s_scores);
+  route_tokens<PER, FULL>(a, begin, end, warp, lane, bias, first, mine, nullptr, s_counts, s_scores);
   if (!counting) return;
   __syncthreads();
   for (int e = threadIdx.x; e < a.E; e += kScoredThreads) {
@@ -404,8 +489,6 @@ route_scored_kernel(const __grid_constant__ ScoredArgs a) {
 }
 
 // ---- the order by expert ----------------------------------------------------------------------
-constexpr int kSortWarps = 16;
-
 // Exclusive prefix over threads (one value each) of a CTA of WARPS warps.
 template <int WARPS>
 __device__ __forceinline__ int cta_prefix(int v, int* s_warp) {
@@ -423,84 +506,31 @@ __device__ __forceinline__ int cta_prefix(int v, int* s_warp) {
   return before;
 }
 
-// counts and prefixes of an expert over the CTAs: a warp per expert, in place.
-__global__ void __launch_bounds__(256)
-scan_hist_kernel(int32_t* hist, int n_ctas, int E, int32_t* counts) {
-  const int e = (int)blockIdx.x * 8 + ((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
-  griddep_launch_dependents();
-  griddep_wait();
-  if (e >= E) return;
-  int32_t* const row = hist + (size_t)e * n_ctas;
-  int carry = 0;
-  for (int i0 = 0; i0 < n_ctas; i0 += 128) {  // four values a lane at a time
-    int v[4], sum = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = i0 + lane * 4 + j;
-      v[j] = i < n_ctas ? row[i] : 0;
-      sum += v[j];
-    }
-    int incl = sum;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, incl, d);
-      if (lane >= d) incl += o;
-    }
-    int at = carry + incl - sum;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = i0 + lane * 4 + j;
-      if (i < n_ctas) row[i] = at;
-      at += v[j];
-    }
-    carry += __shfl_sync(0xffffffffu, incl, 31);
-  }
-  if (lane == 0) counts[e] = carry;
-}
-
-// Rows of one CTA's assignments in the stable order by expert.  hist == nullptr: one CTA has them all and makes the
-// counts too.  Every warp counts the experts of a contiguous part, then hands out its part's rows in order.
-__global__ void __launch_bounds__(kSortWarps * 32)
-place_kernel(const int32_t* __restrict__ ids, int T, int K, int E, int part_tokens, const int32_t* __restrict__ hist,
-             int32_t* counts, int32_t* __restrict__ offsets, int32_t* __restrict__ perm) {
-  extern __shared__ int s_rows[];  // [kSortWarps][E]
-  __shared__ int s_warp[kSortWarps];
-  static_assert(kSortWarps * 32 >= OLED_MAX_EXPERTS, "a thread per expert");
+// Rows of a CTA's n assignments (ids[0 .. n - 1], the first of them number a0) in the stable order by expert.  Every warp counts the
+// experts of a contiguous part (s_rows: [kScoredWarps][E], zeros), start(e, n of the CTA) says where the CTA's rows of an expert
+// begin, and every warp hands out its part's rows in order.
+template <typename Start>
+__device__ __forceinline__ void place_rows(const int32_t* ids, int n, int64_t a0, int E, int* s_rows, int32_t* __restrict__ perm, Start start) {
+  static_assert(kScoredThreads >= OLED_MAX_EXPERTS, "a thread per expert");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  griddep_launch_dependents();
-  for (int i = threadIdx.x; i < kSortWarps * E; i += kSortWarps * 32) s_rows[i] = 0;
-  griddep_wait();
-  __syncthreads();
-  const int64_t a0 = (int64_t)blockIdx.x * part_tokens * K, a1 = min(a0 + (int64_t)part_tokens * K, (int64_t)T * K);
-  const int n = (int)(a1 - a0), per_warp = (n + kSortWarps * 32 - 1) / (kSortWarps * 32) * 32;
-  const int first = warp * per_warp, last = min(n, first + per_warp);
+  const int per_warp = (n + kScoredThreads - 1) / kScoredThreads * 32, first = warp * per_warp, last = min(n, first + per_warp);
   int* const mine = s_rows + warp * E;
-  for (int i0 = first; i0 < last; i0 += 32)
-    if (i0 + lane < last) atomicAdd(&mine[ids[a0 + i0 + lane]], 1);
+  for (int i = first + lane; i < last; i += 32) atomicAdd(&mine[ids[i]], 1);
   __syncthreads();
   const int e = threadIdx.x;
   int total = 0;
-  if (e < E) {
-    for (int w = 0; w < kSortWarps; ++w) {
+  if (e < E)
+    for (int w = 0; w < kScoredWarps; ++w) {
       const int c = s_rows[w * E + e];
       s_rows[w * E + e] = total;
       total += c;
     }
-    if (hist == nullptr) counts[e] = total;
-    else total = counts[e];
-  }
-  int start = cta_prefix<kSortWarps>(e < E ? total : 0, s_warp);
-  if (e < E) {
-    if (blockIdx.x == 0) {
-      offsets[e] = start;
-      if (e == E - 1) offsets[E] = start + total;
-    }
-    if (hist != nullptr) start += hist[(size_t)e * gridDim.x + blockIdx.x];
-    for (int w = 0; w < kSortWarps; ++w) s_rows[w * E + e] += start;
-  }
+  const int at = start(e, total);
+  if (e < E)
+    for (int w = 0; w < kScoredWarps; ++w) s_rows[w * E + e] += at;
   __syncthreads();
   for (int i0 = first; i0 < last; i0 += 32) {
-    const int id = i0 + lane < last ? ids[a0 + i0 + lane] : -1;
+    const int id = i0 + lane < last ? ids[i0 + lane] : -1;
     const uint32_t same = __match_any_sync(0xffffffffu, id);
     const int rank = __popc(same & ((1u << lane) - 1u));
     if (id >= 0) perm[mine[id] + rank] = (int32_t)(a0 + i0 + lane);
@@ -510,15 +540,122 @@ place_kernel(const int32_t* __restrict__ ids, int T, int K, int E, int part_toke
   }
 }
 
-// How many CTAs share a routing of T tokens, and how.  Up to kOneSort assignments are sorted by one CTA, which takes no
-// scratch; beyond, a CTA sorts what it routed and a kernel in between adds up the CTAs' histograms.
-constexpr int kOneSort = 4096;
-constexpr int kScoredCtas = 148 * 4;
-bool one_sort(int T, int K) { return (int64_t)T * K <= kOneSort; }
+constexpr int kScoredCtas = 148 * 2;  // at most
+
+// Counts and prefixes of an expert over the CTAs: a warp per expert, in place, all of its values in flight together.
+__global__ void __launch_bounds__(256)
+scan_hist_kernel(int32_t* hist, int n_ctas, int E, int32_t* counts) {
+  constexpr int kPer = (kScoredCtas + 31) / 32;
+  const int e = (int)blockIdx.x * 8 + ((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
+  griddep_launch_dependents();
+  griddep_wait();
+  if (e >= E) return;
+  int32_t* const row = hist + (size_t)e * n_ctas;
+  int v[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) v[j] = j * 32 + lane < n_ctas ? row[j * 32 + lane] : 0;
+  int carry = 0;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    int incl = v[j];
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += o;
+    }
+    if (j * 32 + lane < n_ctas) row[j * 32 + lane] = carry + incl - v[j];
+    carry += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (lane == 0) counts[e] = carry;
+}
+
+__global__ void __launch_bounds__(kScoredThreads)
+place_kernel(const int32_t* __restrict__ ids, int T, int K, int E, int part_tokens, const int32_t* __restrict__ hist,
+             const int32_t* __restrict__ counts, int32_t* __restrict__ offsets, int32_t* __restrict__ perm) {
+  extern __shared__ int s_rows[];  // [kScoredWarps][E]
+  __shared__ int s_warp[kScoredWarps];
+  griddep_launch_dependents();
+  for (int i = threadIdx.x; i < kScoredWarps * E; i += kScoredThreads) s_rows[i] = 0;
+  griddep_wait();
+  __syncthreads();
+  const int64_t a0 = (int64_t)blockIdx.x * part_tokens * K, a1 = min(a0 + (int64_t)part_tokens * K, (int64_t)T * K);
+  const int mine = (int)threadIdx.x < E ? counts[threadIdx.x] : 0;
+  const int before = (int)threadIdx.x < E ? hist[(size_t)threadIdx.x * gridDim.x + blockIdx.x] : 0;
+  place_rows(ids + a0, (int)(a1 - a0), a0, E, s_rows, perm, [&](int e, int) {
+    const int start = cta_prefix<kScoredWarps>(mine, s_warp);
+    if (blockIdx.x == 0 && e < E) {
+      offsets[e] = start;
+      if (e == E - 1) offsets[E] = start + mine;
+    }
+    return start + before;
+  });
+}
+
+// Few tokens: routing and order in one launch by one cluster of up to eight CTAs, which add up their counts through
+// distributed shared memory.  (A launch costs the caller more than these kernels the GPU.)
+constexpr int kOneLaunch = 4096;                        // assignments
+constexpr int kClusterIds = kOneLaunch / 8 + OLED_MAX_TOPK;  // of a CTA (16 tokens each with fewer than eight CTAs)
+template <int PER, bool FULL>
+__global__ void __launch_bounds__(kScoredThreads)
+route_cluster_kernel(const __grid_constant__ ScoredArgs a, int32_t* __restrict__ counts, int32_t* __restrict__ offsets,
+                     int32_t* __restrict__ perm) {
+  extern __shared__ int s_rows[];  // [kScoredWarps][E]
+  __shared__ int s_total[OLED_MAX_EXPERTS];
+  __shared__ int32_t s_ids[kClusterIds];
+  __shared__ int s_warp[kScoredWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_ctas = gridDim.x, rank = blockIdx.x;
+  griddep_launch_dependents();
+  for (int i = threadIdx.x; i < kScoredWarps * a.E; i += kScoredThreads) s_rows[i] = 0;
+  griddep_wait();
+  int first, mine;
+  float bias[PER];
+  lane_experts<PER>(a, lane, first, mine, bias);
+  const int begin = min(rank * a.part_tokens, a.T), end = min(begin + a.part_tokens, a.T);
+  route_tokens<PER, FULL>(a, begin, end, warp, lane, bias, first, mine, s_ids, nullptr, nullptr);
+  __syncthreads();
+  place_rows(s_ids, (end - begin) * a.K, (int64_t)begin * a.K, a.E, s_rows, perm, [&](int e, int total) {
+    int all = total, before = 0;
+    if (n_ctas > 1) {
+      if (e < a.E) s_total[e] = total;
+      cluster_sync_all();
+      if (e < a.E) {
+        all = 0;
+        const uint32_t at = smem_u32(&s_total[e]);
+        int v[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          if (c < n_ctas) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v[c]) : "r"(map_to_cta(at, (uint32_t)c)) : "memory");
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          if (c < n_ctas) {
+            if (c < rank) before += v[c];
+            all += v[c];
+          }
+      }
+    }
+    const int start = cta_prefix<kScoredWarps>(e < a.E ? all : 0, s_warp);
+    if (rank == 0 && e < a.E) {
+      counts[e] = all;
+      offsets[e] = start;
+      if (e == a.E - 1) offsets[a.E] = start + all;
+    }
+    return start + before;
+  });
+  if (n_ctas > 1) cluster_sync_all();  // nobody leaves while another CTA may still read its counts
+}
+
+// How many CTAs share a routing of T tokens.  Up to kOneLaunch assignments a cluster sorts its own, which takes no scratch;
+// beyond, a CTA sorts what it routed and a kernel in between adds up the CTAs' histograms.
+bool one_launch(int T, int K) { return (int64_t)T * K <= kOneLaunch; }
 int scored_parts(int T) {
   const int parts = std::min((T + kScoredWarps - 1) / kScoredWarps, kScoredCtas);
   const int part_tokens = (T + parts - 1) / parts;
   return (T + part_tokens - 1) / part_tokens;  // (none of them empty)
+}
+int cluster_ctas(int T) {
+  int n = 1;
+  while (n < 8 && n * kScoredWarps < T) n *= 2;
+  return n;
 }
 
 bool routing_ok(const oled_routing* r) {
@@ -552,23 +689,44 @@ ScoredArgs scored_args(const oled_routing& r, const float* logits, int64_t strid
   // (a token that may use every group has no use for them)
   if (a.top_groups == a.G) a.G = a.top_groups = 1;
   a.group_size = a.E / a.G;
-  int lanes = 32;
-  while (32 / lanes < a.G) lanes >>= 1;
-  a.lanes_per_group = lanes;
+  a.lanes_log2 = 5;
+  while ((32 >> a.lanes_log2) < a.G) --a.lanes_log2;
+  const int lanes = a.lanes_per_group = 1 << a.lanes_log2;
   a.per_lane = (a.group_size + lanes - 1) / lanes;
   // 16-byte loads where every lane's experts are whole vectors on 16-byte boundaries
   a.vec = a.per_lane % 4 == 0 && a.group_size % 4 == 0 && stride % 4 == 0 && !off_boundary(logits, 16);
   return a;
 }
 
+// Calls f with the kernel's PER and FULL as constants.
+template <typename F>
+cudaError_t with_layout(const ScoredArgs& a, F f) {
+  // FULL: as many lanes as there are have as many experts as the kernel has room for
+  const bool full = a.lanes_per_group * a.G == 32 && a.per_lane * a.lanes_per_group == a.group_size;
+  using std::integral_constant;
+  auto pick = [&](auto per) {
+    if (full && a.per_lane == decltype(per)::value) return f(per, integral_constant<bool, true>{});
+    return f(per, integral_constant<bool, false>{});
+  };
+  if (a.per_lane <= 2) return pick(integral_constant<int, 2>{});
+  if (a.per_lane <= 4) return pick(integral_constant<int, 4>{});
+  if (a.per_lane <= 8) return pick(integral_constant<int, 8>{});
+  if (a.per_lane <= 16) return pick(integral_constant<int, 16>{});
+  return f(integral_constant<int, 32>{}, integral_constant<bool, false>{});  // (full lanes have 16 experts at most)
+}
+
 cudaError_t launch_scored(cudaStream_t st, const ScoredArgs& a, int ctas) {
   const size_t smem = (a.scores != nullptr ? (size_t)a.E * 8 : 0) + (a.hist != nullptr || a.counts != nullptr ? (size_t)a.E * 4 : 0);
-  const dim3 grid((unsigned)ctas), block(kScoredThreads);
-  if (a.per_lane <= 2) return launch_pdl(route_scored_kernel<2>, grid, block, smem, st, a);
-  if (a.per_lane <= 4) return launch_pdl(route_scored_kernel<4>, grid, block, smem, st, a);
-  if (a.per_lane <= 8) return launch_pdl(route_scored_kernel<8>, grid, block, smem, st, a);
-  if (a.per_lane <= 16) return launch_pdl(route_scored_kernel<16>, grid, block, smem, st, a);
-  return launch_pdl(route_scored_kernel<32>, grid, block, smem, st, a);
+  return with_layout(a, [&](auto per, auto full) {
+    return launch_pdl(route_scored_kernel<decltype(per)::value, decltype(full)::value>, dim3((unsigned)ctas), dim3(kScoredThreads), smem, st, a);
+  });
+}
+
+cudaError_t launch_route_cluster(cudaStream_t st, const ScoredArgs& a, int ctas, int32_t* counts, int32_t* offsets, int32_t* perm) {
+  return with_layout(a, [&](auto per, auto full) {
+    return launch_cluster(route_cluster_kernel<decltype(per)::value, decltype(full)::value>, dim3((unsigned)ctas), dim3(kScoredThreads),
+                          (size_t)kScoredWarps * a.E * sizeof(int), st, ctas, a, counts, offsets, perm);
+  });
 }
 
 }  // namespace
@@ -600,7 +758,7 @@ cudaError_t launch_route_step(cudaStream_t st, const oled_routing& r, const floa
 
 extern "C" size_t oled_route_scored_scratch(const oled_routing* routing, int32_t n_tokens) {
   using namespace oled;
-  if (!routing_ok(routing) || n_tokens <= 0 || n_tokens > OLED_MAX_ROUTE_TOKENS || one_sort(n_tokens, routing->top_k)) return 0;
+  if (!routing_ok(routing) || n_tokens <= 0 || n_tokens > OLED_MAX_ROUTE_TOKENS || one_launch(n_tokens, routing->top_k)) return 0;
   return (size_t)scored_parts(n_tokens) * (size_t)routing->n_experts * sizeof(int32_t);
 }
 
@@ -626,7 +784,7 @@ extern "C" int oled_route_scored(const oled_routing* routing, const float* logit
     return OLED_OK;
   }
   if (!logits || !ids || !gate) return OLED_ERR_INVALID_ARG;
-  const bool whole = !order || one_sort(T, K);
+  const bool whole = !order || one_launch(T, K);
   if (!whole && (!scratch || scratch_bytes < oled_route_scored_scratch(routing, T))) return OLED_ERR_INVALID_ARG;
   {
     const int64_t n = (int64_t)T * K * 4;
@@ -638,21 +796,23 @@ extern "C" int oled_route_scored(const oled_routing* routing, const float* logit
         if (rows_overlap(r[i], r[j])) return OLED_ERR_INVALID_ARG;
   }
   ScoredArgs a = scored_args(*routing, logits, logits_stride, bias, T, ids, gate);
-  a.parts = scored_parts(T);
   a.seg_tokens = T;
-  a.part_tokens = (T + a.parts - 1) / a.parts;
-  if (!whole) a.hist = static_cast<int32_t*>(scratch);
-  cudaError_t err = launch_scored(st, a, a.parts);
-  const size_t smem = (size_t)kSortWarps * E * sizeof(int);
-  // (each of these indexes by what the one before has stored: it is launched only behind one that was)
-  if (err == cudaSuccess && order && whole)
-    err = launch_pdl(place_kernel, dim3(1), dim3(kSortWarps * 32), smem, st, (const int32_t*)ids, T, K, E, T, (const int32_t*)nullptr,
-                     counts, offsets, perm);
-  if (err == cudaSuccess && order && !whole) {
-    err = launch_pdl(scan_hist_kernel, dim3((unsigned)((E + 7) / 8)), dim3(256), 0, st, a.hist, a.parts, E, counts);
-    if (err == cudaSuccess)
-      err = launch_pdl(place_kernel, dim3((unsigned)a.parts), dim3(kSortWarps * 32), smem, st, (const int32_t*)ids, T, K, E,
-                       a.part_tokens, (const int32_t*)a.hist, counts, offsets, perm);
+  cudaError_t err;
+  if (order && whole) {
+    const int ctas = cluster_ctas(T);
+    a.part_tokens = (T + ctas - 1) / ctas;
+    err = launch_route_cluster(st, a, ctas, counts, offsets, perm);
+  } else {
+    a.parts = scored_parts(T);
+    a.part_tokens = (T + a.parts - 1) / a.parts;
+    if (order) a.hist = static_cast<int32_t*>(scratch);
+    err = launch_scored(st, a, a.parts);
+    // (each of these indexes by what the one before has stored: it is launched only behind one that was)
+    if (err == cudaSuccess && order)
+      err = launch_pdl(scan_hist_kernel, dim3((unsigned)((E + 7) / 8)), dim3(256), 0, st, a.hist, a.parts, E, counts);
+    if (err == cudaSuccess && order)
+      err = launch_pdl(place_kernel, dim3((unsigned)a.parts), dim3(kScoredThreads), (size_t)kScoredWarps * E * sizeof(int), st,
+                       (const int32_t*)ids, T, K, E, a.part_tokens, (const int32_t*)a.hist, (const int32_t*)counts, offsets, perm);
   }
   return cudaGetLastError() == cudaSuccess && err == cudaSuccess ? OLED_OK : OLED_ERR_CUDA;
 }
