@@ -6,9 +6,9 @@
 // Everything between the loads and the stores is fp32, and every output is rounded once: h is made from x' itself, not
 // from its bf16 form.
 //
-// Bound by HBM (4096 bf16 columns: 8 bytes an element).  A row stays in the registers of one CTA (of one warp up to 256
-// columns) between the two sums that it needs, eight consecutive values per thread and vector, so that sixteen
-// lanes hold a block of 128.
+// Bound by HBM (8 bytes an element where all is bf16; 16384 x 4096 with an fp32 stream 6.55 TB/s, as much as a copy).  A row stays in
+// the registers of one CTA (of one warp up to 512 columns) between the two sums that it needs, eight consecutive values per
+// thread and vector, so that sixteen lanes hold a block of 128.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -36,60 +36,44 @@ struct NormArgs {
   float eps, scale;
 };
 
-// Eight values at column c of a row, zeros behind its end.  VEC: rows are whole 16-byte vectors on 16-byte boundaries.
-template <bool VEC>
-__device__ __forceinline__ void load8(const uint16_t* row, int c, int hidden, float (&v)[8]) {
-  if (VEC) {
-    uint4 p = make_uint4(0u, 0u, 0u, 0u);
-    if (c < hidden) p = *reinterpret_cast<const uint4*>(row + c);
-    unpack8(p, v);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < hidden ? __uint_as_float((uint32_t)row[c + j] << 16) : 0.0f;
+// Eight values at column c of a row, zeros behind its end, as they lie in memory.
+struct Raw16 {
+  uint4 p;
+  __device__ __forceinline__ void values(float (&v)[8]) const { unpack8(p, v); }
+};
+struct Raw32 {
+  uint4 p, q;
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    v[0] = __uint_as_float(p.x); v[1] = __uint_as_float(p.y); v[2] = __uint_as_float(p.z); v[3] = __uint_as_float(p.w);
+    v[4] = __uint_as_float(q.x); v[5] = __uint_as_float(q.y); v[6] = __uint_as_float(q.z); v[7] = __uint_as_float(q.w);
   }
+};
+__device__ __forceinline__ Raw16 load8(const uint16_t* row, int c, int hidden) {
+  Raw16 r{make_uint4(0u, 0u, 0u, 0u)};
+  if (c < hidden) r.p = *reinterpret_cast<const uint4*>(row + c);
+  return r;
 }
-template <bool VEC>
-__device__ __forceinline__ void load8(const float* row, int c, int hidden, float (&v)[8]) {
-  if (VEC) {
-    float4 p = make_float4(0.f, 0.f, 0.f, 0.f), q = p;
-    if (c < hidden) {
-      p = *reinterpret_cast<const float4*>(row + c);
-      q = *reinterpret_cast<const float4*>(row + c + 4);
-    }
-    v[0] = p.x; v[1] = p.y; v[2] = p.z; v[3] = p.w;
-    v[4] = q.x; v[5] = q.y; v[6] = q.z; v[7] = q.w;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < hidden ? row[c + j] : 0.0f;
+__device__ __forceinline__ Raw32 load8(const float* row, int c, int hidden) {
+  Raw32 r{make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+  if (c < hidden) {
+    r.p = *reinterpret_cast<const uint4*>(row + c);
+    r.q = *reinterpret_cast<const uint4*>(row + c + 4);
   }
+  return r;
 }
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-template <bool VEC>
 __device__ __forceinline__ void store8(uint16_t* row, int c, int hidden, const float (&v)[8]) {
-  if (VEC) {
-    if (c < hidden)
-      *reinterpret_cast<uint4*>(row + c) =
-          make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (c + j < hidden) row[c + j] = __bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
-  }
+  if (c < hidden)
+    *reinterpret_cast<uint4*>(row + c) =
+        make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
 }
-template <bool VEC>
 __device__ __forceinline__ void store8(float* row, int c, int hidden, const float (&v)[8]) {
-  if (VEC) {
-    if (c < hidden) {
-      *reinterpret_cast<float4*>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(row + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (c + j < hidden) row[c + j] = v[j];
+  if (c < hidden) {
+    *reinterpret_cast<float4*>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(row + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
   }
 }
 
@@ -109,8 +93,10 @@ __device__ __forceinline__ float row_sum(float s, float* s_part) {
   return s;
 }
 
-// R: the residual stream's type (uint16_t: bf16).  THREADS per row (32: four rows per CTA), V vectors per thread.
-template <typename R, int THREADS, int V, bool VEC>
+// Rows of whole 16-byte vectors on 16-byte boundaries (codes: on 8-byte boundaries).
+// R: the residual stream's type (uint16_t: bf16).  THREADS per row (32: four rows per CTA), V vectors per thread.  Two vectors
+// were best wherever there are threads for it (16384 x 2048 bf16 with codes: 54 us, one vector 66, four 63).
+template <typename R, int THREADS, int V>
 __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS)
 norm_kernel(const __grid_constant__ NormArgs a) {
   __shared__ float s_part[2][THREADS / 32];
@@ -121,49 +107,67 @@ norm_kernel(const __grid_constant__ NormArgs a) {
   griddep_wait();
   if (t >= a.tokens) return;  // (whole warps, and only where no barrier follows)
   const R* const xr = static_cast<const R*>(a.x) + t * a.x_stride;
+  const uint16_t* const yr = a.y + t * a.y_stride;
+  const uint16_t* const gr = a.gate + (a.gate_tokens > 0 ? t / a.gate_tokens : 0) * a.gate_stride;
+  // Everything that the row needs is requested before its first sum - the weights too where x is bf16 (16384 x 4096: 95.7 us,
+  // with them 88.1); beside an fp32 x their registers cost more warps than that saves (122.6 us, with them 136.9).
+  constexpr bool kEarly = sizeof(R) == 2;
+  decltype(load8(xr, 0, 0)) x_raw[V];
+  Raw16 y_raw[V], post[V], gate[V], pre[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int c = (lane_in_row + i * THREADS) * 8;
+    if (a.y != nullptr) y_raw[i] = load8(yr, c, H);
+    x_raw[i] = load8(xr, c, H);
+  }
+  if (kEarly)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int c = (lane_in_row + i * THREADS) * 8;
+      if (a.post != nullptr) post[i] = load8(a.post, c, H);
+      if (a.gate != nullptr) gate[i] = load8(gr, c, H);
+      if (a.pre != nullptr) pre[i] = load8(a.pre, c, H);
+    }
   float v[V][8];
-#pragma unroll
-  for (int i = 0; i < V; ++i) load8<VEC>(xr, (lane_in_row + i * THREADS) * 8, H, v[i]);
   if (a.y != nullptr) {
-    float z[V][8];
-    const uint16_t* const yr = a.y + t * a.y_stride;
+    float z[V][8], r = 1.0f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) load8<VEC>(yr, (lane_in_row + i * THREADS) * 8, H, z[i]);
-    float f = a.scale;
+    for (int i = 0; i < V; ++i) y_raw[i].values(z[i]);
     if (a.post != nullptr) {
       float s = 0.0f;
 #pragma unroll
       for (int i = 0; i < V; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) s = fmaf(z[i][j], z[i][j], s);
-      const float r = rsqrtf(row_sum<THREADS>(s, s_part[0]) / (float)H + a.eps);
+      r = rsqrtf(row_sum<THREADS>(s, s_part[0]) / (float)H + a.eps);
+    }
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float w[8];
-        load8<VEC>(a.post, (lane_in_row + i * THREADS) * 8, H, w);
+    for (int i = 0; i < V; ++i) {
+      float w[8];
+      if (a.post != nullptr) {
+        if (!kEarly) post[i] = load8(a.post, (lane_in_row + i * THREADS) * 8, H);
+        post[i].values(w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) z[i][j] = z[i][j] * r * w[j];
       }
-    }
-    if (a.gate != nullptr) {
-      const uint16_t* const gr = a.gate + (a.gate_tokens > 0 ? t / a.gate_tokens : 0) * a.gate_stride;
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        float w[8];
-        load8<VEC>(gr, (lane_in_row + i * THREADS) * 8, H, w);
+      if (a.gate != nullptr) {
+        if (!kEarly) gate[i] = load8(gr, (lane_in_row + i * THREADS) * 8, H);
+        gate[i].values(w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) z[i][j] *= w[j];
       }
+      x_raw[i].values(v[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = fmaf(a.scale, z[i][j], v[i][j]);
     }
+  } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] = fmaf(f, z[i][j], v[i][j]);
+    for (int i = 0; i < V; ++i) x_raw[i].values(v[i]);
   }
   if (a.x_out != nullptr) {
     R* const xo = static_cast<R*>(a.x_out) + t * a.x_out_stride;
 #pragma unroll
-    for (int i = 0; i < V; ++i) store8<VEC>(xo, (lane_in_row + i * THREADS) * 8, H, v[i]);
+    for (int i = 0; i < V; ++i) store8(xo, (lane_in_row + i * THREADS) * 8, H, v[i]);
   }
   if (a.pre == nullptr) return;
   float s = 0.0f;
@@ -176,35 +180,115 @@ norm_kernel(const __grid_constant__ NormArgs a) {
   for (int i = 0; i < V; ++i) {
     const int c = (lane_in_row + i * THREADS) * 8;
     float w[8];
-    load8<VEC>(a.pre, c, H, w);
+    if (!kEarly) pre[i] = load8(a.pre, c, H);
+    pre[i].values(w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * r * w[j];
-    if (a.h != nullptr) store8<VEC>(a.h + t * a.h_stride, c, H, v[i]);
+    if (a.h != nullptr) store8(a.h + t * a.h_stride, c, H, v[i]);
     if (a.codes != nullptr) {
       const uint32_t amax = amax_half_warp(amax8(v[i]));
       const uint2 q = codes8(v[i], block_inverse(amax));
       uint8_t* const cr = a.codes + t * a.codes_stride;
-      if (VEC) {
-        if (c < H) *reinterpret_cast<uint2*>(cr + c) = q;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (c + j < H) cr[c + j] = (uint8_t)((j < 4 ? q.x : q.y) >> (8 * (j & 3)));
-      }
+      if (c < H) *reinterpret_cast<uint2*>(cr + c) = q;
       if ((threadIdx.x & 15) == 0 && c < H) a.scales[t * a.scales_stride + c / kScaleBlock] = block_scale(amax);
     }
   }
 }
 
-template <typename R, bool VEC>
-cudaError_t launch_norm_kind(cudaStream_t st, const NormArgs& a) {
-  const dim3 row((unsigned)a.tokens);
-  if (a.hidden <= 256) return launch_pdl(norm_kernel<R, 32, 1, VEC>, dim3((unsigned)((a.tokens + 3) / 4)), dim3(128), 0, st, a);
-  if (a.hidden <= 1024) return launch_pdl(norm_kernel<R, 128, 1, VEC>, row, dim3(128), 0, st, a);
-  if (a.hidden <= 2048) return launch_pdl(norm_kernel<R, 256, 1, VEC>, row, dim3(256), 0, st, a);
-  if (a.hidden <= 4096) return launch_pdl(norm_kernel<R, 256, 2, VEC>, row, dim3(256), 0, st, a);
-  if (a.hidden <= 8192) return launch_pdl(norm_kernel<R, 512, 2, VEC>, row, dim3(512), 0, st, a);
-  return launch_pdl(norm_kernel<R, 512, 4, VEC>, row, dim3(512), 0, st, a);
+// Any other rows: element by element, a warp's 32 next to each other, N per thread.  A block of 128 is then four warps'
+// elements of one turn.  (Eight consecutive elements a thread, loaded one by one, took 168 us at 4099 x 3759.)
+__device__ __forceinline__ float load1(const uint16_t* row, int c) { return __uint_as_float((uint32_t)row[c] << 16); }
+__device__ __forceinline__ float load1(const float* row, int c) { return row[c]; }
+__device__ __forceinline__ void store1(uint16_t* row, int c, float v) { row[c] = __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
+__device__ __forceinline__ void store1(float* row, int c, float v) { row[c] = v; }
+
+template <typename R, int THREADS, int N>
+__global__ void __launch_bounds__(THREADS)
+norm_odd_kernel(const __grid_constant__ NormArgs a) {
+  __shared__ float s_part[2][THREADS / 32];
+  __shared__ uint32_t s_amax[N][THREADS / 32];
+  const int H = a.hidden, tid = threadIdx.x;
+  const int64_t t = blockIdx.x;
+  griddep_launch_dependents();
+  griddep_wait();
+  const R* const xr = static_cast<const R*>(a.x) + t * a.x_stride;
+  float v[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = tid + i * THREADS < H ? load1(xr, tid + i * THREADS) : 0.0f;
+  if (a.y != nullptr) {
+    const uint16_t* const yr = a.y + t * a.y_stride;
+    const uint16_t* const gr = a.gate + (a.gate_tokens > 0 ? t / a.gate_tokens : 0) * a.gate_stride;
+    float z[N], r = 1.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = tid + i * THREADS < H ? load1(yr, tid + i * THREADS) : 0.0f;
+    if (a.post != nullptr) {
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) s = fmaf(z[i], z[i], s);
+      r = rsqrtf(row_sum<THREADS>(s, s_part[0]) / (float)H + a.eps);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = tid + i * THREADS;
+      if (c >= H) continue;
+      if (a.post != nullptr) z[i] = z[i] * r * load1(a.post, c);
+      if (a.gate != nullptr) z[i] *= load1(gr, c);
+      v[i] = fmaf(a.scale, z[i], v[i]);
+    }
+  }
+  if (a.x_out != nullptr) {
+    R* const xo = static_cast<R*>(a.x_out) + t * a.x_out_stride;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (tid + i * THREADS < H) store1(xo, tid + i * THREADS, v[i]);
+  }
+  if (a.pre == nullptr) return;
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) s = fmaf(v[i], v[i], s);
+  const float r = rsqrtf(row_sum<THREADS>(s, s_part[1]) / (float)H + a.eps);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = tid + i * THREADS;
+    if (c < H) {
+      v[i] = v[i] * r * load1(a.pre, c);
+      if (a.h != nullptr) store1(a.h + t * a.h_stride, c, v[i]);
+    }
+    if (a.codes != nullptr) {
+      const uint32_t big = __reduce_max_sync(0xffffffffu, c < H ? __float_as_uint(v[i]) & 0x7fffffffu : 0u);
+      if ((tid & 31) == 0) s_amax[i][tid >> 5] = big;
+    }
+  }
+  if (a.codes == nullptr) return;
+  __syncthreads();
+  uint8_t* const cr = a.codes + t * a.codes_stride;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = tid + i * THREADS;
+    if (c >= H) continue;
+    const uint32_t* const four = &s_amax[i][(tid >> 7) * 4];
+    const uint32_t amax = max(max(max(four[0], four[1]), max(four[2], four[3])), kAmaxFloor);
+    cr[c] = (uint8_t)e4m3x2(__fmul_rn(v[i], block_inverse(amax)), 0.0f);
+    if ((tid & 127) == 0) a.scales[t * a.scales_stride + c / kScaleBlock] = block_scale(amax);
+  }
+}
+
+template <typename R>
+cudaError_t launch_norm_kind(cudaStream_t st, const NormArgs& a, bool vec) {
+  const dim3 row((unsigned)a.tokens), rows4((unsigned)((a.tokens + 3) / 4));
+  if (!vec) {
+    if (a.hidden <= 512) return launch_pdl(norm_odd_kernel<R, 128, 4>, row, dim3(128), 0, st, a);
+    if (a.hidden <= 2048) return launch_pdl(norm_odd_kernel<R, 256, 8>, row, dim3(256), 0, st, a);
+    if (a.hidden <= 4096) return launch_pdl(norm_odd_kernel<R, 256, 16>, row, dim3(256), 0, st, a);
+    return launch_pdl(norm_odd_kernel<R, 512, 32>, row, dim3(512), 0, st, a);
+  }
+  if (a.hidden <= 256) return launch_pdl(norm_kernel<R, 32, 1>, rows4, dim3(128), 0, st, a);
+  if (a.hidden <= 512) return launch_pdl(norm_kernel<R, 32, 2>, rows4, dim3(128), 0, st, a);
+  if (a.hidden <= 1024) return launch_pdl(norm_kernel<R, 64, 2>, row, dim3(64), 0, st, a);
+  if (a.hidden <= 2048) return launch_pdl(norm_kernel<R, 128, 2>, row, dim3(128), 0, st, a);
+  if (a.hidden <= 4096) return launch_pdl(norm_kernel<R, 256, 2>, row, dim3(256), 0, st, a);
+  if (a.hidden <= 8192) return launch_pdl(norm_kernel<R, 512, 2>, row, dim3(512), 0, st, a);
+  return launch_pdl(norm_kernel<R, 512, 4>, row, dim3(512), 0, st, a);
 }
 
 }  // namespace
@@ -277,9 +361,7 @@ int norm_residual(const oled_norm_shape* shape, const void* x, const void* y, co
   rows_ok(pre_weight, 0, 16);
   rows_ok(h, s.h_stride * 2, 16);
   rows_ok(h_codes, s.codes_stride, 8);
-  cudaError_t err;
-  if (s.residual == OLED_FP32) err = vec ? launch_norm_kind<float, true>(st, a) : launch_norm_kind<float, false>(st, a);
-  else err = vec ? launch_norm_kind<uint16_t, true>(st, a) : launch_norm_kind<uint16_t, false>(st, a);
+  const cudaError_t err = s.residual == OLED_FP32 ? launch_norm_kind<float>(st, a, vec) : launch_norm_kind<uint16_t>(st, a, vec);
   return cudaGetLastError() == cudaSuccess && err == cudaSuccess ? OLED_OK : OLED_ERR_CUDA;
 }
 

@@ -2,8 +2,9 @@
 // bf16 rows or of silu(gate) * up of rows gate | up, in fp32 from the loads to the codes.
 //
 // Bound by HBM: 2 bytes read (4 with SwiGLU) and 1 written per element.  A half-warp holds a block, eight values (one
-// 16-byte load) a lane, so that a block's maximum is four shuffles; a warp takes 1024 columns of a row at a time, its
-// four loads (eight with SwiGLU) in flight together.
+// 16-byte load) a lane, so that a block's maximum is four shuffles; a warp takes VECS times 256 columns of a row, its
+// loads in flight together: four of them where there are rows enough to fill the GPU (16384 x 4096: 35.2 us, two 37.5), one where
+// there are not (32 x 1024 with SwiGLU 1.9 us, four 2.6).
 #include <algorithm>
 
 #include "block_scale.h"
@@ -13,11 +14,9 @@
 namespace oled {
 namespace {
 
-constexpr int kQuantWarps = 8;
-constexpr int kQuantVecs = 4;                          // 16-byte vectors a lane has in flight
-constexpr int kQuantCols = kQuantVecs * 32 * 8;        // columns of a warp's piece
+constexpr int kQuantWarps = 4;
 
-template <bool SWIGLU>
+template <bool SWIGLU, int VECS>
 __global__ void __launch_bounds__(kQuantWarps * 32)
 quantize_kernel(const uint16_t* __restrict__ x, int64_t x_stride, int64_t pieces, int pieces_per_row, int cols,
                 uint8_t* __restrict__ codes, int64_t codes_stride, float* __restrict__ scales, int64_t scales_stride) {
@@ -27,11 +26,11 @@ quantize_kernel(const uint16_t* __restrict__ x, int64_t x_stride, int64_t pieces
   const int64_t piece = (int64_t)blockIdx.x * kQuantWarps + (threadIdx.x >> 5);
   if (piece >= pieces) return;
   const int64_t row = pieces_per_row == 1 ? piece : piece / pieces_per_row;
-  const int c0 = (int)(piece - row * pieces_per_row) * kQuantCols + lane * 8;
+  const int c0 = (int)(piece - row * pieces_per_row) * (VECS * 256) + lane * 8;
   const uint16_t* src = x + row * x_stride + c0;
-  uint4 a[kQuantVecs], b[SWIGLU ? kQuantVecs : 1];
+  uint4 a[VECS], b[SWIGLU ? VECS : 1];
 #pragma unroll
-  for (int i = 0; i < kQuantVecs; ++i) {
+  for (int i = 0; i < VECS; ++i) {
     a[i] = make_uint4(0u, 0u, 0u, 0u);
     if (SWIGLU) b[i] = a[i];
     if (c0 + i * 256 < cols) {  // (cols is a multiple of 16: a vector is whole or absent)
@@ -40,7 +39,7 @@ quantize_kernel(const uint16_t* __restrict__ x, int64_t x_stride, int64_t pieces
     }
   }
 #pragma unroll
-  for (int i = 0; i < kQuantVecs; ++i) {
+  for (int i = 0; i < VECS; ++i) {
     float v[8];
     unpack8(a[i], v);
     if (SWIGLU) {
@@ -63,11 +62,13 @@ quantize_kernel(const uint16_t* __restrict__ x, int64_t x_stride, int64_t pieces
 
 cudaError_t launch_quantize(cudaStream_t st, const uint16_t* x, int64_t x_stride, int64_t rows, int cols, bool swiglu,
                             uint8_t* codes, int64_t codes_stride, float* scales, int64_t scales_stride) {
-  const int per_row = (cols + kQuantCols - 1) / kQuantCols;
+  // four vectors a lane once that still gives every SM sixteen warps
+  const bool wide = rows * ((cols + 1023) / 1024) >= 148 * 16;
+  const int width = wide ? 1024 : 256, per_row = (cols + width - 1) / width;
   const int64_t pieces = rows * per_row;
   const dim3 grid((unsigned)((pieces + kQuantWarps - 1) / kQuantWarps));
-  return launch_pdl(swiglu ? quantize_kernel<true> : quantize_kernel<false>, grid, dim3(kQuantWarps * 32), 0, st, x, x_stride,
-                    pieces, per_row, cols, codes, codes_stride, scales, scales_stride);
+  const auto kernel = swiglu ? (wide ? quantize_kernel<true, 4> : quantize_kernel<true, 1>) : (wide ? quantize_kernel<false, 4> : quantize_kernel<false, 1>);
+  return launch_pdl(kernel, grid, dim3(kQuantWarps * 32), 0, st, x, x_stride, pieces, per_row, cols, codes, codes_stride, scales, scales_stride);
 }
 
 }  // namespace oled
