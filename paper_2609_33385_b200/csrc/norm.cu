@@ -196,7 +196,8 @@ norm_kernel(const __grid_constant__ NormArgs a) {
 }
 
 // Any other rows: element by element, a warp's 32 next to each other, N per thread.  A block of 128 is then four warps'
-// elements of one turn.  (Eight consecutive elements a thread, loaded one by one, took 168 us at 4099 x 3759.)
+// elements of one turn.  (Eight consecutive elements a thread, loaded one by one, took 168 us at
+// 4099 x 3759 with both outputs, 16 of these 133, eight 66; the code of a row is run once, and fetching it counts.)
 __device__ __forceinline__ float load1(const uint16_t* row, int c) { return __uint_as_float((uint32_t)row[c] << 16); }
 __device__ __forceinline__ float load1(const float* row, int c) { return row[c]; }
 __device__ __forceinline__ void store1(uint16_t* row, int c, float v) { row[c] = __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
@@ -262,14 +263,18 @@ norm_odd_kernel(const __grid_constant__ NormArgs a) {
   if (a.codes == nullptr) return;
   __syncthreads();
   uint8_t* const cr = a.codes + t * a.codes_stride;
+  // lane i has the scale of the block that the warp's elements of turn i belong to
+  static_assert(N <= 32, "a lane per turn");
+  const int lane = tid & 31, turn = min(lane, N - 1), block = ((tid & ~127) + turn * THREADS) / kScaleBlock;
+  const uint32_t* const four = &s_amax[turn][(tid >> 7) * 4];
+  const uint32_t amax = max(max(max(four[0], four[1]), max(four[2], four[3])), kAmaxFloor);
+  const float inverse = block_inverse(amax);
+  if ((tid & 127) < N && block * kScaleBlock < H) a.scales[t * a.scales_stride + block] = block_scale(amax);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
+    const float f = __shfl_sync(0xffffffffu, inverse, i);
     const int c = tid + i * THREADS;
-    if (c >= H) continue;
-    const uint32_t* const four = &s_amax[i][(tid >> 7) * 4];
-    const uint32_t amax = max(max(max(four[0], four[1]), max(four[2], four[3])), kAmaxFloor);
-    cr[c] = (uint8_t)e4m3x2(__fmul_rn(v[i], block_inverse(amax)), 0.0f);
-    if ((tid & 127) == 0) a.scales[t * a.scales_stride + c / kScaleBlock] = block_scale(amax);
+    if (c < H) cr[c] = (uint8_t)e4m3x2(__fmul_rn(v[i], f), 0.0f);
   }
 }
 
@@ -279,8 +284,9 @@ cudaError_t launch_norm_kind(cudaStream_t st, const NormArgs& a, bool vec) {
   if (!vec) {
     if (a.hidden <= 512) return launch_pdl(norm_odd_kernel<R, 128, 4>, row, dim3(128), 0, st, a);
     if (a.hidden <= 2048) return launch_pdl(norm_odd_kernel<R, 256, 8>, row, dim3(256), 0, st, a);
-    if (a.hidden <= 4096) return launch_pdl(norm_odd_kernel<R, 256, 16>, row, dim3(256), 0, st, a);
-    return launch_pdl(norm_odd_kernel<R, 512, 32>, row, dim3(512), 0, st, a);
+    if (a.hidden <= 4096) return launch_pdl(norm_odd_kernel<R, 512, 8>, row, dim3(512), 0, st, a);
+    if (a.hidden <= 8192) return launch_pdl(norm_odd_kernel<R, 1024, 8>, row, dim3(1024), 0, st, a);
+    return launch_pdl(norm_odd_kernel<R, 1024, 16>, row, dim3(1024), 0, st, a);
   }
   if (a.hidden <= 256) return launch_pdl(norm_kernel<R, 32, 1>, rows4, dim3(128), 0, st, a);
   if (a.hidden <= 512) return launch_pdl(norm_kernel<R, 32, 2>, rows4, dim3(128), 0, st, a);
