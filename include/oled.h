@@ -459,6 +459,44 @@ typedef struct {
 int oled_matmul_blocks(const oled_product_shape* shape, const void* a, const float* a_scale, const void* b,
                           const float* b_scale, const void* add, int32_t m, void* cuda_stream, void* out);
 
+/* ---- the same operators inside a context's steps ----------------------------------------------------
+ * Each layer may have any of them; a NULL description takes a layer's away again.  Calls synchronise the context's
+ * stream; nothing is changed by a call that fails.  Device memory that the steps then need (for norms max_tokens rows of
+ * hidden values, for a shared expert its operands) is allocated by the first such call: OOM if it is not to be had.
+ *
+ * The layer's routing: steps choose experts and weights from the layer's gate logits as oled_route_scored() does, with
+ * n_experts and top_k of the context; score_bias: fp32[E], host or device, copied, or NULL.  The reuse scores take the weights
+ * before `scale`.  (Such a step sorts its rows; few-token steps of other layers bring them to their experts in the gate kernel.) */
+int oled_register_routing(oled_ctx* ctx, int32_t layer, const oled_routing* routing, const float* score_bias);
+
+/* The norms around the layer in oled_denoise_iteration(): its input is h = rms(x) * pre_weight (pre_weight NULL: x), and
+ * x' = x + residual_scale * gate * (rms(out) * post_weight) (gate, post_weight NULL: without them) the next layer's x; see
+ * oled_norm_residual().  The last layer's x' is the iteration's result.  Device arrays bf16[hidden], gate rows
+ * bf16[ceil(n_tokens / gate_tokens)][hidden] (gate_tokens 0: one row), borrowed, 2-byte aligned.  oled_denoise_step() is not affected. */
+typedef struct {
+  const void* pre_weight;
+  const void* post_weight;
+  const void* gate;
+  int32_t gate_tokens;
+  float eps;             /* > 0 */
+  float residual_scale;
+} oled_layer_norms;
+int oled_register_norms(oled_ctx* ctx, int32_t layer, const oled_layer_norms* norms);
+
+/* The layer's shared expert, which every token takes beside its routed ones: out = bf16(routed) + down(silu(gate) * up), all of
+ * its products of e4m3 codes with block scales, the layer's input and the activations quantised on the way
+ * (oled_quantize_blocks(), oled_matmul_blocks()).  gate_up: codes [2 * intermediate, hidden], gate rows first, scales
+ * fp32 [2 * intermediate / 128, hidden / 128]; down: codes [hidden, intermediate], scales fp32 [hidden / 128, intermediate / 128].
+ * Device arrays, borrowed; codes 16-byte aligned; intermediate a multiple of 128, at most OLED_MAX_PRODUCT_K. */
+typedef struct {
+  int32_t intermediate;
+  const void* gate_up;
+  const float* gate_up_scale;
+  const void* down;
+  const float* down_scale;
+} oled_shared_expert;
+int oled_register_shared_expert(oled_ctx* ctx, int32_t layer, const oled_shared_expert* expert);
+
 /* ---- host-only policy simulator (no GPU needed): the same C++ policy code the step uses,
  * driven by recorded counts and integer scores.  For tests of the host logic. ---- */
 typedef struct oled_policy oled_policy;

@@ -47,7 +47,8 @@ EXPORTS = [
     "oled_policy_adapt", "oled_clear_status", "oled_policy_time", "oled_expert_blob_bytes",
     "oled_self_check_report", "oled_debug_perm", "oled_policy_create_stack", "oled_debug_timeline",
     "oled_policy_tile_rows", "oled_route_scored", "oled_route_scored_scratch", "oled_norm_residual",
-    "oled_quantize_blocks", "oled_matmul_blocks",
+    "oled_quantize_blocks", "oled_matmul_blocks", "oled_register_routing", "oled_register_norms",
+    "oled_register_shared_expert",
 ]
 EXPERTS_BF16, EXPERTS_FP8 = 0, 1
 NOALLOC_MAX_TOKENS = 256
@@ -84,6 +85,18 @@ class ProductShape(C.Structure):
     """``oled_product_shape``; strides count elements."""
     _fields_ = [("n", C.c_int32), ("k", C.c_int32), ("out", C.c_int32)] + [(n, C.c_int64) for n in (
         "a_stride", "a_scale_stride", "b_stride", "b_scale_stride", "add_stride", "out_stride")]
+
+
+class LayerNorms(C.Structure):
+    """``oled_layer_norms``: device pointers (None: absent)."""
+    _fields_ = [("pre_weight", C.c_void_p), ("post_weight", C.c_void_p), ("gate", C.c_void_p), ("gate_tokens", C.c_int32),
+                ("eps", C.c_float), ("residual_scale", C.c_float)]
+
+
+class SharedExpert(C.Structure):
+    """``oled_shared_expert``: device pointers."""
+    _fields_ = [("intermediate", C.c_int32), ("gate_up", C.c_void_p), ("gate_up_scale", C.c_void_p), ("down", C.c_void_p),
+                ("down_scale", C.c_void_p)]
 
 
 class KernelProfile(C.Structure):
@@ -181,6 +194,9 @@ def load() -> C.CDLL:
     lib.oled_norm_residual.argtypes = [C.POINTER(NormShape), vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp]
     lib.oled_quantize_blocks.argtypes = [vp, i64, i32, i32, i32, vp, vp, i64, vp, i64]
     lib.oled_matmul_blocks.argtypes = [C.POINTER(ProductShape), vp, vp, vp, vp, vp, i32, vp, vp]
+    lib.oled_register_routing.argtypes = [vp, i32, C.POINTER(Routing), vp]
+    lib.oled_register_norms.argtypes = [vp, i32, C.POINTER(LayerNorms)]
+    lib.oled_register_shared_expert.argtypes = [vp, i32, C.POINTER(SharedExpert)]
     _lib = lib
     return lib
 
@@ -224,6 +240,15 @@ class OledContext:
     def register_experts(self, layer: int, host_blob_ptr: int, expert_stride_bytes: int) -> None:
         self._check(self._lib.oled_register_experts(self._h, layer, host_blob_ptr,
                                                     expert_stride_bytes), "oled_register_experts")
+
+    def register_routing(self, layer: int, routing: Optional[Routing], score_bias_ptr: Optional[int] = None) -> None:
+        self._check(self._lib.oled_register_routing(self._h, layer, routing, score_bias_ptr), "oled_register_routing")
+
+    def register_norms(self, layer: int, norms: Optional[LayerNorms]) -> None:
+        self._check(self._lib.oled_register_norms(self._h, layer, norms), "oled_register_norms")
+
+    def register_shared_expert(self, layer: int, expert: Optional[SharedExpert]) -> None:
+        self._check(self._lib.oled_register_shared_expert(self._h, layer, expert), "oled_register_shared_expert")
 
     def denoise_step(self, layer: int, hidden_ptr: int, conf_ptr: int, n_tokens: int,
                      out_ptr: int) -> None:

@@ -205,7 +205,8 @@ void launch_route(cudaStream_t st, const uint16_t* x, const uint16_t* w_router, 
                   const float* conf, int T, int H, int E, int K, float* logits, int32_t* ids,
                   float* gate, int32_t* counts, unsigned long long* scores, const CombinePrev& prev,
                   StepTimeline* timeline, int32_t* seg_counts = nullptr, int seg_tokens = 0,
-                  const ScatterRows& scatter = ScatterRows{});
+                  const ScatterRows& scatter = ScatterRows{}, bool logits_only = false);
+// logits_only: the logits and a CombinePrev, but no choice (launch_route_step makes it).
 // Does the gate kernel of a T-token step carry out a CombinePrev and a ScatterRows?
 bool route_staged(int T, int K);
 constexpr int kDenseTokens = 32;
@@ -351,7 +352,8 @@ int launch_ffn_few(cudaStream_t st, const FfnTcMaps& maps, const FfnGroup& grp, 
 // ---- operators without a context (norm.cu, quantize.cu, product.cu, route_scored.cu): the entry points' bodies, which
 // check their arguments, and launches that take checked ones ----------------------------------
 int norm_residual(const oled_norm_shape* shape, const void* x, const void* y, const void* post_weight, const void* gate,
-                  const void* pre_weight, int32_t n_tokens, cudaStream_t st, void* x_out, void* h, void* h_codes, float* h_scales);
+                  const void* pre_weight, int32_t n_tokens, cudaStream_t st, void* x_out, void* h, void* h_codes, float* h_scales,
+                  float pre_eps);  // (of the second norm; 0: the shape's)
 cudaError_t launch_quantize(cudaStream_t st, const uint16_t* x, int64_t x_stride, int64_t rows, int cols, bool swiglu,
                             uint8_t* codes, int64_t codes_stride, float* scales, int64_t scales_stride);
 int matmul_blocks(const oled_product_shape* shape, const void* a, const float* a_scale, const void* b, const float* b_scale,

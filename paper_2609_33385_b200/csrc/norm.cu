@@ -33,7 +33,7 @@ struct NormArgs {
   float* scales;
   int64_t x_stride, y_stride, gate_stride, x_out_stride, h_stride, codes_stride, scales_stride;
   int tokens, hidden, gate_tokens;
-  float eps, scale;
+  float eps, pre_eps, scale;
 };
 
 // Eight values at column c of a row, zeros behind its end, as they lie in memory.
@@ -175,7 +175,7 @@ norm_kernel(const __grid_constant__ NormArgs a) {
   for (int i = 0; i < V; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) s = fmaf(v[i][j], v[i][j], s);
-  const float r = rsqrtf(row_sum<THREADS>(s, s_part[1]) / (float)H + a.eps);
+  const float r = rsqrtf(row_sum<THREADS>(s, s_part[1]) / (float)H + a.pre_eps);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int c = (lane_in_row + i * THREADS) * 8;
@@ -247,7 +247,7 @@ norm_odd_kernel(const __grid_constant__ NormArgs a) {
   float s = 0.0f;
 #pragma unroll
   for (int i = 0; i < N; ++i) s = fmaf(v[i], v[i], s);
-  const float r = rsqrtf(row_sum<THREADS>(s, s_part[1]) / (float)H + a.eps);
+  const float r = rsqrtf(row_sum<THREADS>(s, s_part[1]) / (float)H + a.pre_eps);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int c = tid + i * THREADS;
@@ -300,7 +300,7 @@ cudaError_t launch_norm_kind(cudaStream_t st, const NormArgs& a, bool vec) {
 }  // namespace
 
 int norm_residual(const oled_norm_shape* shape, const void* x, const void* y, const void* post_weight, const void* gate,
-                  const void* pre_weight, int32_t n_tokens, cudaStream_t st, void* x_out, void* h, void* h_codes, float* h_scales) {
+                  const void* pre_weight, int32_t n_tokens, cudaStream_t st, void* x_out, void* h, void* h_codes, float* h_scales, float pre_eps) {
   if (!shape) return OLED_ERR_INVALID_ARG;
   const oled_norm_shape& s = *shape;
   const int H = s.hidden, blocks = (H + kScaleBlock - 1) / kScaleBlock;
@@ -353,6 +353,7 @@ int norm_residual(const oled_norm_shape* shape, const void* x, const void* y, co
   a.hidden = H;
   a.gate_tokens = s.gate_tokens;
   a.eps = s.eps;
+  a.pre_eps = pre_eps > 0.0f ? pre_eps : s.eps;
   a.scale = s.residual_scale;
   // 16-byte vectors where every row that is touched starts on a 16-byte boundary (codes: 8) and holds whole ones
   bool vec = H % 8 == 0;
@@ -377,5 +378,5 @@ extern "C" int oled_norm_residual(const oled_norm_shape* shape, const void* x, c
                                   const void* gate, const void* pre_weight, int32_t n_tokens, void* cuda_stream, void* x_out,
                                   void* h, void* h_codes, float* h_scales) {
   return oled::norm_residual(shape, x, y, post_weight, gate, pre_weight, n_tokens, static_cast<cudaStream_t>(cuda_stream), x_out, h,
-                             h_codes, h_scales);
+                             h_codes, h_scales, 0.0f);
 }

@@ -31,6 +31,15 @@ struct LayerData {
   uint16_t* w_router = nullptr;  // device [E,H]
   float* bias = nullptr;         // device [E] or null
   bool has_router = false;
+  // what stands around the routed experts (each may be absent)
+  bool scored = false;           // routing of its own
+  oled_routing routing{};
+  float* score_bias = nullptr;   // device [E], the context's; has_score_bias: in use
+  bool has_score_bias = false;
+  bool has_norms = false;
+  oled_layer_norms norms{};
+  bool has_shared = false;
+  oled_shared_expert shared{};
   oled_stats_t stats{};
 };
 
@@ -112,6 +121,15 @@ struct oled_ctx {
   float* d_conf_stage = nullptr;
   uint16_t* d_out_stage = nullptr;
   uint16_t* d_iter[2] = {nullptr, nullptr};  // ping-pong hidden states of the stack iteration
+  uint16_t* d_norm = nullptr;          // [T,H] a layer's normed input (allocated with the first norms)
+  // a shared expert's operands (allocated with the first one, for the largest intermediate size so far)
+  uint8_t* shared_memory = nullptr;
+  int shared_intermediate = 0;
+  uint8_t* d_shared_codes = nullptr;   // [T,H] codes of the layer's input, and their scales [T,H/128]
+  float* d_shared_scales = nullptr;
+  uint16_t* d_shared_mid = nullptr;    // [T,2I] gate | up
+  uint8_t* d_shared_act = nullptr;     // [T,I] codes of silu(gate) * up, and their scales [T,I/128]
+  float* d_shared_act_scales = nullptr;
   // pinned host mirror of the control block
   uint8_t* h_ctrl = nullptr;
   uint32_t* h_status = nullptr;
@@ -268,6 +286,8 @@ void free_ctx(oled_ctx* ctx) {
   if (!ctx) return;
   if (ctx->stream || ctx->copy_stream) cudaDeviceSynchronize();
   cudaFree(ctx->device_memory);
+  cudaFree(ctx->d_norm);
+  cudaFree(ctx->shared_memory);
   if (ctx->h_ctrl) cudaFreeHost(ctx->h_ctrl);
   if (ctx->h_status) cudaFreeHost(ctx->h_status);
   for (auto ev : ctx->fill_events) cudaEventDestroy(ev);
@@ -628,6 +648,7 @@ int oled_create(const oled_model_shape* shape, const int32_t* cache_capacity, vo
     for (int l = 0; l < s.n_layers; ++l) {
       mem.add(&ctx->layers[l].w_router, E * H);
       if (s.has_router_bias) mem.add(&ctx->layers[l].bias, E);
+      mem.add(&ctx->layers[l].score_bias, E);
     }
     mem.add(&ctx->d_counts_copy, E);
     rc = mem.allocate(ctx);
@@ -703,6 +724,104 @@ int oled_register_experts(oled_ctx* ctx, int32_t layer, const void* host_blob, s
   L.host_blob = static_cast<const uint8_t*>(host_blob);
   L.host_stride = expert_stride_bytes;
   return OLED_OK;
+}
+
+int oled_register_routing(oled_ctx* ctx, int32_t layer, const oled_routing* routing, const float* score_bias) {
+  if (!ctx || layer < 0 || layer >= ctx->shape.n_layers || misaligned(score_bias, 4)) return OLED_ERR_INVALID_ARG;
+  if (routing ? (!routing_valid(routing) || routing->n_experts != ctx->shape.n_experts || routing->top_k != ctx->shape.top_k)
+              : score_bias != nullptr)
+    return OLED_ERR_INVALID_ARG;
+  LayerData& L = ctx->layers[layer];
+  OLED_CUDA(ctx, cudaStreamSynchronize(ctx->stream));
+  if (score_bias) {
+    OLED_CUDA(ctx, cudaMemcpyAsync(L.score_bias, score_bias, (size_t)ctx->shape.n_experts * sizeof(float), cudaMemcpyDefault, ctx->stream));
+    OLED_CUDA(ctx, cudaStreamSynchronize(ctx->stream));
+  }
+  L.scored = routing != nullptr;
+  if (routing) L.routing = *routing;
+  L.has_score_bias = score_bias != nullptr;
+  return OLED_OK;
+}
+
+int oled_register_norms(oled_ctx* ctx, int32_t layer, const oled_layer_norms* norms) {
+  if (!ctx || layer < 0 || layer >= ctx->shape.n_layers) return OLED_ERR_INVALID_ARG;
+  if (norms && (norms->gate_tokens < 0 || !(norms->eps > 0.0f) || !std::isfinite(norms->eps) || !std::isfinite(norms->residual_scale) ||
+                misaligned(norms->pre_weight, 2) || misaligned(norms->post_weight, 2) || misaligned(norms->gate, 2)))
+    return OLED_ERR_INVALID_ARG;
+  OLED_CUDA(ctx, cudaStreamSynchronize(ctx->stream));
+  if (norms && ctx->d_norm == nullptr &&
+      cudaMalloc(reinterpret_cast<void**>(&ctx->d_norm), (size_t)ctx->shape.max_tokens * ctx->shape.hidden * 2) != cudaSuccess) {
+    cudaGetLastError();
+    ctx->d_norm = nullptr;
+    return OLED_ERR_OOM;
+  }
+  LayerData& L = ctx->layers[layer];
+  L.has_norms = norms != nullptr;
+  if (norms) L.norms = *norms;
+  return OLED_OK;
+}
+
+int oled_register_shared_expert(oled_ctx* ctx, int32_t layer, const oled_shared_expert* expert) {
+  if (!ctx || layer < 0 || layer >= ctx->shape.n_layers) return OLED_ERR_INVALID_ARG;
+  if (expert) {
+    const oled_shared_expert& x = *expert;
+    if (x.intermediate <= 0 || x.intermediate % 128 != 0 || x.intermediate > OLED_MAX_PRODUCT_K || !x.gate_up || !x.gate_up_scale || !x.down ||
+        !x.down_scale || misaligned(x.gate_up, 16) || misaligned(x.down, 16) || misaligned(x.gate_up_scale, 4) || misaligned(x.down_scale, 4))
+      return OLED_ERR_INVALID_ARG;
+  }
+  OLED_CUDA(ctx, cudaStreamSynchronize(ctx->stream));
+  if (expert && expert->intermediate > ctx->shared_intermediate) {
+    const size_t T = (size_t)ctx->shape.max_tokens, H = (size_t)ctx->shape.hidden, I = (size_t)expert->intermediate;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+      const size_t offset = at;
+      at += (bytes + 255) / 256 * 256;
+      return offset;
+    };
+    const size_t codes = take(T * H), scales = take(T * (H / 128) * 4), mid = take(T * 2 * I * 2), act = take(T * I), act_scales = take(T * (I / 128) * 4);
+    uint8_t* memory = nullptr;
+    if (cudaMalloc(reinterpret_cast<void**>(&memory), at) != cudaSuccess) {
+      cudaGetLastError();
+      return OLED_ERR_OOM;
+    }
+    cudaFree(ctx->shared_memory);
+    ctx->shared_memory = memory;
+    ctx->shared_intermediate = expert->intermediate;
+    ctx->d_shared_codes = memory + codes;
+    ctx->d_shared_scales = reinterpret_cast<float*>(memory + scales);
+    ctx->d_shared_mid = reinterpret_cast<uint16_t*>(memory + mid);
+    ctx->d_shared_act = memory + act;
+    ctx->d_shared_act_scales = reinterpret_cast<float*>(memory + act_scales);
+  }
+  LayerData& L = ctx->layers[layer];
+  L.has_shared = expert != nullptr;
+  if (expert) L.shared = *expert;
+  return OLED_OK;
+}
+
+// The shared expert of a step, up to the codes of its activations.
+static int shared_expert_up(oled_ctx* ctx, const LayerData& L, const void* hidden, int T) {
+  NvtxRange nv(ctx, "oled.step.shared_expert_up");
+  const int H = ctx->shape.hidden, I = L.shared.intermediate;
+  OLED_CUDA(ctx, launch_quantize(ctx->stream, static_cast<const uint16_t*>(hidden), H, T, H, false, ctx->d_shared_codes, H, ctx->d_shared_scales,
+                                 H / 128));
+  oled_product_shape up{2 * I, H, OLED_BF16, H, H / 128, H, H / 128, 0, 2 * I};
+  const int rc = matmul_blocks(&up, ctx->d_shared_codes, ctx->d_shared_scales, L.shared.gate_up, L.shared.gate_up_scale, nullptr, T, ctx->stream,
+                               ctx->d_shared_mid);
+  if (rc != OLED_OK) return rc;
+  OLED_CUDA(ctx, launch_quantize(ctx->stream, ctx->d_shared_mid, 2 * I, T, I, true, ctx->d_shared_act, I, ctx->d_shared_act_scales, I / 128));
+  ctx->launches += 3;
+  return OLED_OK;
+}
+
+// ... and its down projection, added to the routed experts' sum in `out`.
+static int shared_expert_down(oled_ctx* ctx, const LayerData& L, int T, void* out) {
+  NvtxRange nv(ctx, "oled.step.shared_expert_down");
+  const int H = ctx->shape.hidden, I = L.shared.intermediate;
+  oled_product_shape down{H, I, OLED_BF16, I, I / 128, I, I / 128, H, H};
+  const int rc = matmul_blocks(&down, ctx->d_shared_act, ctx->d_shared_act_scales, L.shared.down, L.shared.down_scale, out, T, ctx->stream, out);
+  ctx->launches += 1;
+  return rc;
 }
 
 // x_next != nullptr: also write x_next = bf16(hidden + out), the residual between layers.
@@ -782,7 +901,7 @@ static int step_impl(oled_ctx* ctx, int32_t layer, const void* hidden, const flo
   ctx->scatter = ScatterRows{};
   ctx->perm_stale = false;
   ctx->step_split = nullptr;
-  if (few && route_staged(T, K) && (size_t)E * scatter_cap(T) <= ctx->row_buf && ctx->ffn_impl == 0 &&
+  if (few && !L.scored && route_staged(T, K) && (size_t)E * scatter_cap(T) <= ctx->row_buf && ctx->ffn_impl == 0 &&
       !ctx->corrupt_perm) {
     ctx->scatter.cap = (int)scatter_cap(T);
     ctx->scatter.assignment = ctx->d_assignment;
@@ -817,7 +936,12 @@ static int step_impl(oled_ctx* ctx, int32_t layer, const void* hidden, const flo
     }
     launch_route(st, static_cast<const uint16_t*>(hidden), L.w_router, L.bias, confidences, T, H, E, K,
                  ctx->d_logits, ctx->d_ids, ctx->d_gate, ctx->d_counts, ctx->d_scores, prev, tl, seg_counts, seg_tokens,
-                 ctx->scatter);
+                 ctx->scatter, L.scored);
+    if (L.scored) {
+      OLED_CUDA(ctx, launch_route_step(st, L.routing, ctx->d_logits, L.has_score_bias ? L.score_bias : nullptr, confidences, T, ctx->d_ids,
+                                       ctx->d_gate, ctx->d_counts, ctx->d_scores, seg_counts, seg_tokens));
+      ctx->launches += 1;
+    }
   }
   // Many rows per expert (every FFN launch of the step on CTA pairs, token tiles of 256 rows): no
   // gather kernel, each gate/up launch copies its experts' token rows while its first items run.
@@ -900,6 +1024,10 @@ static int step_impl(oled_ctx* ctx, int32_t layer, const void* hidden, const flo
   }
 
   nv_ffn_hits.end();
+  if (L.has_shared) {  // (its first product and the activations run while the host plans)
+    const int rcs = shared_expert_up(ctx, L, hidden, T);
+    if (rcs != OLED_OK) return rcs;
+  }
   NvtxRange nv_policy(ctx, "oled.step.5_reuse_score_retention_fills");
   // The report implies that everything enqueued before this step has completed, so slots
   // released earlier are free to be overwritten by the side stream.
@@ -990,7 +1118,7 @@ static int step_impl(oled_ctx* ctx, int32_t layer, const void* hidden, const flo
   nv_ffn_miss.end();
   NvtxRange nv_comb(ctx, "oled.step.4_combine");
   // 5. combine - or, inside a stack iteration of few-token steps, left to the next layer's gate kernel
-  const bool defer = defer_combine && ctx->fuse_combine && route_staged(T, K) && x_next != nullptr &&
+  const bool defer = defer_combine && !L.has_shared && ctx->fuse_combine && route_staged(T, K) && x_next != nullptr &&
                      !ctx->y_bf16 && !ctx->self_check && ctx->ffn_impl == 0;
   if (defer) {
     ctx->pending.valid = true;
@@ -1007,10 +1135,19 @@ static int step_impl(oled_ctx* ctx, int32_t layer, const void* hidden, const flo
       ProfScope ps(ctx, OLED_KERNEL_COMBINE, (uint64_t)T * K * H * (ctx->y_bf16 ? 2 : 4) + (uint64_t)T * H * 2,
                    2ull * T * K * H);
       launch_combine(st, ctx->d_y, ctx->y_bf16 ? 1 : 0, ctx->d_gate, scattered ? nullptr : ctx->d_pos, T, H, K, static_cast<uint16_t*>(out),
-                     static_cast<const uint16_t*>(hidden), static_cast<uint16_t*>(x_next),
+                     static_cast<const uint16_t*>(hidden), L.has_shared ? nullptr : static_cast<uint16_t*>(x_next),
                      reinterpret_cast<uint32_t*>(ctx->d_scores), (int)(ctx->ctrl_bytes / 4), tl);
     }
     ctx->launches += 1;
+    if (L.has_shared) {
+      const int rcs = shared_expert_down(ctx, L, T, out);
+      if (rcs != OLED_OK) return rcs;
+      if (x_next != nullptr) {
+        launch_residual_add(st, static_cast<const uint16_t*>(hidden), static_cast<const uint16_t*>(out), static_cast<uint16_t*>(x_next),
+                            (size_t)T * H);
+        ctx->launches += 1;
+      }
+    }
     if (ctx->self_check) {
       launch_guard_check(st, ctx->guards, ctx->d_status);
       ctx->launches += 1;
@@ -1107,19 +1244,63 @@ static int prefetch_next_layer(oled_ctx* ctx, int32_t next) {
   return OLED_OK;
 }
 
+// Between two layers of a stack with norms: x_out = x + scale * gate * norm(y) as the layer `done` has it (x alone in front of the
+// first one), and into d_norm the input of the layer `next` (nullptr: its input is x_out).
+static int norm_between(oled_ctx* ctx, const LayerData* done, const LayerData* next, const void* x, const void* y, int32_t n_tokens, void* x_out) {
+  const int H = ctx->shape.hidden;
+  oled_norm_shape s{};
+  s.hidden = H;
+  s.residual = OLED_BF16;
+  s.eps = 1.0f;
+  s.residual_scale = 1.0f;
+  s.x_stride = s.y_stride = s.gate_stride = s.x_out_stride = s.h_stride = H;
+  const void *post = nullptr, *gate = nullptr;
+  if (done && done->has_norms) {
+    s.eps = done->norms.eps;
+    s.residual_scale = done->norms.residual_scale;
+    s.gate_tokens = done->norms.gate_tokens;
+    post = done->norms.post_weight;
+    gate = done->norms.gate;
+  }
+  const int rc = norm_residual(&s, x, y, post, gate, next ? next->norms.pre_weight : nullptr, n_tokens, ctx->stream, x_out,
+                               next ? ctx->d_norm : nullptr, nullptr, nullptr, next ? next->norms.eps : 0.0f);
+  ctx->launches += 1;
+  return rc;
+}
+
 int oled_denoise_iteration(oled_ctx* ctx, const void* hidden, const float* confidences, int32_t n_tokens,
                            void* hidden_out) {
   if (!ctx || n_tokens < 0) return OLED_ERR_INVALID_ARG;
   if (n_tokens > ctx->shape.max_tokens) return OLED_ERR_TOO_MANY_TOKENS;
   if (n_tokens > 0 && (!hidden || !confidences || !hidden_out)) return OLED_ERR_INVALID_ARG;
   const void* x = hidden;
-  for (int l = 0; l < ctx->shape.n_layers; ++l) {
-    void* nxt = (l + 1 == ctx->shape.n_layers) ? hidden_out : (void*)ctx->d_iter[l & 1];
-    const int rc = step_impl(ctx, l, x, confidences, n_tokens, ctx->d_out_stage, nxt, l + 1 < ctx->shape.n_layers);
+  const int last = ctx->shape.n_layers - 1;
+  bool normed = false;
+  for (const LayerData& L : ctx->layers) normed = normed || L.has_norms;
+  if (normed && (misaligned(hidden, 16) || misaligned(hidden_out, 16))) return OLED_ERR_INVALID_ARG;
+  // a layer's input: its x, or that normed
+  auto normed_input = [&](int l) { return ctx->layers[l].has_norms && ctx->layers[l].norms.pre_weight != nullptr; };
+  if (normed && n_tokens > 0 && normed_input(0)) {
+    const int rc = norm_between(ctx, nullptr, &ctx->layers[0], x, nullptr, n_tokens, nullptr);
     if (rc != OLED_OK) return rc;
+  }
+  for (int l = 0; l <= last; ++l) {
+    void* nxt = l == last ? hidden_out : (void*)ctx->d_iter[l & 1];
+    if (!normed) {
+      const int rc = step_impl(ctx, l, x, confidences, n_tokens, ctx->d_out_stage, nxt, l < last);
+      if (rc != OLED_OK) return rc;
+    } else {
+      const int rc = step_impl(ctx, l, normed_input(l) ? ctx->d_norm : x, confidences, n_tokens, ctx->d_out_stage, nullptr);
+      if (rc != OLED_OK) return rc;
+      if (n_tokens > 0) {
+        const int rcn = norm_between(ctx, &ctx->layers[l], l < last && normed_input(l + 1) ? &ctx->layers[l + 1] : nullptr, x, ctx->d_out_stage,
+                                     n_tokens, nxt);
+        if (rcn != OLED_OK) return rcn;
+      }
+    }
     x = nxt;
     {  // (behind the last layer: the first layer of the iteration that is likely to follow)
-      const int rcp = prefetch_next_layer(ctx, l + 1 < ctx->shape.n_layers ? l + 1 : 0);
+      const int rcp = prefetch_next_layer(ctx, l < last ? l + 1 : 0);
       if (rcp != OLED_OK) return rcp;
     }
   }

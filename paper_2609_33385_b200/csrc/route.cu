@@ -419,7 +419,7 @@ route_kernel(const uint16_t* __restrict__ x, const uint16_t* __restrict__ wr,
   }
   __syncthreads();
 
-  if (staged) {
+  if (staged && K > 0) {
     // top-k by rank: expert e is selected iff fewer than K experts precede it in the order (logit descending,
     // index ascending), and its rank is the number that do.  `parts` neighbouring threads per (token, expert)
     // count a share of the experts each, four keys at a time.  (A warp per expert at a time took 1.4 us for
@@ -508,7 +508,7 @@ route_kernel(const uint16_t* __restrict__ x, const uint16_t* __restrict__ wr,
         }
       }
     }
-  } else {
+  } else if (!staged) {
     // one warp per token
     for (int a = warp; a < TT; a += kRouteWarps) {
       const int t = t0 + a;
@@ -669,7 +669,7 @@ route_many_kernel(const uint16_t* __restrict__ x, const uint16_t* __restrict__ w
   // the experts' words receives one addition per CTA: with one per assignment the few words of the popular experts were
   // a queue (4096 tokens, 64 experts top-8: 89 us, now 81; a batch of 1000 tokens in 4 layers 808 us, now 795).
   const int seg0 = seg_counts != nullptr ? t0 / seg_tokens : 0;
-  for (int a = warp; a < TT; a += kManyWarps) {
+  for (int a = warp; a < TT && K > 0; a += kManyWarps) {
     const int t = t0 + a;
     if (t >= T) continue;
     const int second = seg_counts != nullptr && t >= (seg0 + 1) * seg_tokens ? E : 0;
@@ -957,8 +957,10 @@ bool route_staged(int T, int K) { return T <= 296 || (T <= 1024 && (size_t)T * K
 void launch_route(cudaStream_t st, const uint16_t* x, const uint16_t* w_router, const float* bias,
                   const float* conf, int T, int H, int E, int K, float* logits, int32_t* ids,
                   float* gate, int32_t* counts, unsigned long long* scores, const CombinePrev& prev,
-                  StepTimeline* timeline, int32_t* seg_counts, int seg_tokens, const ScatterRows& scatter) {
-  if (route_staged(T, K)) {
+                  StepTimeline* timeline, int32_t* seg_counts, int seg_tokens, const ScatterRows& scatter, bool logits_only) {
+  const bool staged = route_staged(T, K);
+  if (logits_only) K = 0;  // (the kernels choose none)
+  if (staged) {
     constexpr int W = kStagedWarps;
     staged_attributes();
     // (the matrix is the context's copy, whose writer has been waited for: it is older than all that may still run on the stream)
