@@ -304,7 +304,7 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
 constexpr int kManyEpiWarps = 8, kManyProducer = 8, kManyMma = 9, kManyThreads = 12 * 32;
 // Registers a thread: 168 at launch (12 warps), of which the third warpgroup gives to the two that accumulate: 4 x 56 + 8 x 224 = 12 x 168.
 constexpr int kManyFewRegs = 56, kManyEpiRegs = 224;
-constexpr int kManyStages = 5, kManyRows = 256, kManyCols = 256;  // of a pair's tile
+constexpr int kManyStages = 4, kManyRows = 256, kManyCols = 256;  // of a pair's tile
 constexpr uint32_t kManyStage = 2 * kWTile;
 constexpr uint32_t kManyOut = 8192;  // staging of a warp's results: 32 rows x 128 bytes, twice
 
@@ -319,7 +319,7 @@ struct __align__(16) ProductManyCtl {
 constexpr uint32_t kManySmem = 1024 + kManyStages * kManyStage + kManyEpiWarps * kManyOut + 1024;
 static_assert(sizeof(ProductManyCtl) <= 1024, "control block");
 
-// The pair's tiles are dealt out in turn (tile t of pair t mod pairs), rows of A first: the pairs of a moment share rows of B.
+// The tiles are dealt out in turn (tile t to pair t mod pairs), along a row of C first (the other way 1 % slower).
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kManyThreads, 1)
 product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a,
                     const __grid_constant__ CUtensorMap map_out, const __grid_constant__ ProductArgs p, int bulk_out) {
@@ -329,7 +329,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_cta_rank();
   const int pair = (int)blockIdx.x >> 1, n_pairs = (int)gridDim.x >> 1;
-  const int tiles_m = (p.m + kManyRows - 1) / kManyRows, tiles = tiles_m * ((p.n + kManyCols - 1) / kManyCols);
+  const int tiles_n = (p.n + kManyCols - 1) / kManyCols, tiles = (p.m + kManyRows - 1) / kManyRows * tiles_n;
   const int kbs = p.k_blocks;
   volatile int* const abort_flag = &ctl->abort;
 
@@ -371,7 +371,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
     int stage = 0;
     uint32_t phase = 0;
     for (int tile = pair; tile < tiles && ok; tile += n_pairs) {
-      const int row_a = (tile % tiles_m) * kManyRows + (int)rank * 128, row_b = (tile / tiles_m) * kManyCols + (int)rank * 128;
+      const int row_a = (tile / tiles_n) * kManyRows + (int)rank * 128, row_b = (tile % tiles_n) * kManyCols + (int)rank * 128;
       for (int kb = 0; kb < kbs; ++kb) {
         ok = product_warp_wait(smem_u32(&ctl->empty[stage]), phase ^ 1u, abort_flag);
         if (!ok) break;
@@ -429,12 +429,12 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
     const int quarter = warp & 3, half = warp >> 2;
     const uint32_t t_row = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
     const uint32_t stage_out = ring + kManyStages * kManyStage + (uint32_t)warp * kManyOut;
-    bool ok = true;
+    bool ok = true, ready = false;
     int buf = 0;
     uint32_t acc_phase = 0;
     for (int tile = pair; tile < tiles; tile += n_pairs) {
-      const int row = (tile % tiles_m) * kManyRows + (int)rank * 128 + quarter * 32 + lane;
-      const int col0 = (tile / tiles_m) * kManyCols + half * 128;
+      const int row = (tile / tiles_n) * kManyRows + (int)rank * 128 + quarter * 32 + lane;
+      const int col0 = (tile % tiles_n) * kManyCols + half * 128;
       const float* const sa = p.a_scale + (int64_t)min(row, p.m - 1) * p.a_scale_stride;
       const float* const sb = p.b_scale + (int64_t)(min(col0, p.n - 1) / 128) * p.b_scale_stride;
       float acc[128];
@@ -448,7 +448,9 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
         s_b = next_b;
         next_a = __ldg(sa + min(kb + 2, kbs - 1));
         next_b = __ldg(sb + min(kb + 2, kbs - 1));
-        ok = product_warp_wait(smem_u32(&ctl->acc_full[buf]), acc_phase, abort_flag);
+        // 64 columns, then 64: the buffer is handed back before its last ones are added, and the next one's barrier is asked
+        // meanwhile (an answer takes 100 cycles even where it is yes)
+        if (!ready) ok = product_warp_wait(smem_u32(&ctl->acc_full[buf]), acc_phase, abort_flag);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
@@ -456,16 +458,18 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
           uint32_t v[64];
           tmem_ld64(t_row + (uint32_t)(buf * kManyCols + q * 64), v);
           tmem_ld_wait();
-          if (q == 1) {  // the buffer is handed back before its last columns are added
+          if (q == 1) {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster_relaxed(acc_empty_on_first + (uint32_t)buf * 8u);
+            buf ^= 1;
+            if (buf == 0) acc_phase ^= 1u;
+            ready = mbar_test(smem_u32(&ctl->acc_full[buf]), acc_phase);
           }
 #pragma unroll
           for (int c = 0; c < 64; ++c) acc[q * 64 + c] = fmaf(__uint_as_float(v[c]), s, acc[q * 64 + c]);
         }
-        buf ^= 1;
-        if (buf == 0) acc_phase ^= 1u;
+        ready = __all_sync(0xffffffffu, ready);
       }
       if (!ok) {
 #pragma unroll

@@ -123,49 +123,42 @@ __device__ __forceinline__ double reciprocal_double(double x) {
   return y;
 }
 
-// The choice of one token in fp64, by the warp that holds its logits: lane r < K ends with the id of rank r.  Scores below
-// exp(-708) count as that.  Few tokens come here, but a CTA waits for the last of its own: four experts of a lane side by side (with
-// exp() and quotients one after the other a token took 5.5 us).  The arrays lie in local memory, since registers count for the whole kernel.
+// The choice of one token in fp64, by the warp that holds its logits: lane r < K ends with the id of rank r.  mask: the lane's experts
+// that can be among the K.  groups: the groups are chosen again too (all experts are in the masks then).  Scores below exp(-708)
+// count as that.  Few tokens come here, but a CTA waits for the last of its own; what they cost is fp64 latency, so only those
+// experts are computed that the fp32 forms leave in question (with all of them a token took 5.5 us).
 template <int PER>
-__device__ __noinline__ int select_exact(const ScoredArgs& a, const float* row, int lane, int first, int mine, float top) {
-  constexpr int kSide = PER < 4 ? PER : 4;
+__device__ __noinline__ int select_exact(const ScoredArgs& a, const float* row, int lane, int first, int mine, float top, uint32_t mask,
+                                         bool groups) {
   const double kNone = -INFINITY;
-  double value[PER];             // exponentials
-  unsigned long long key[PER];   // of the choices, 0: not to be had
-  float logit[PER], bias[PER];   // (all of them requested at once)
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    logit[i] = i < mine ? row[first + i] : 0.0f;
-    bias[i] = i < mine && a.bias != nullptr ? a.bias[first + i] : 0.0f;
-  }
-  double sum = 0.0;
+  unsigned long long key[PER];  // of the choices (in local memory: registers count for the whole kernel)
+  double sum = 1.0;
+  if (a.softmax) {
+    sum = 0.0;
 #pragma unroll 1
-  for (int i0 = 0; i0 < mine; i0 += kSide)
-#pragma unroll
-    for (int i = i0; i < i0 + kSide; ++i) {
-      const float l = no_nan(logit[i]);
-      const double e = exp_double(a.softmax ? (l == top ? 0.0 : (double)l - (double)top) : -(double)l);
-      value[i] = e;
-      if (i < mine) sum += e;
+    for (int i = 0; i < mine; ++i) {
+      const float l = no_nan(row[first + i]);
+      sum += exp_double(l == top ? 0.0 : (double)l - (double)top);
     }
-  for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  }
   double t1 = kNone, t2 = kNone;
 #pragma unroll 1
-  for (int i0 = 0; i0 < mine; i0 += kSide)
-#pragma unroll
-    for (int i = i0; i < i0 + kSide; ++i) {
-      const float l = logit[i];
-      const double score = (a.softmax ? value[i] : 1.0) * reciprocal_double(a.softmax ? sum : 1.0 + value[i]);
-      double c = a.bias == nullptr ? (double)l : score + (double)bias[i];
-      if (!(l == l) || !(c == c)) c = kNone;
-      key[i] = order_key64(c + 0.0);
-      if (i < mine) {
-        const double v = a.bias != nullptr || a.group_top == 1 ? c : score;
-        t2 = fmax(t2, fmin(t1, v));
-        t1 = fmax(t1, v);
-      }
+  for (uint32_t m = mask; m != 0u; m &= m - 1u) {
+    const int i = __ffs((int)m) - 1;
+    const float l = row[first + i], x = no_nan(l);
+    const double e = exp_double(a.softmax ? (x == top ? 0.0 : (double)x - (double)top) : -(double)x);
+    const double score = (a.softmax ? e : 1.0) * reciprocal_double(a.softmax ? sum : 1.0 + e);
+    double c = a.bias == nullptr ? (double)l : score + (double)a.bias[first + i];
+    if (!(l == l) || !(c == c)) c = kNone;
+    key[i] = order_key64(c + 0.0);
+    if (groups) {
+      const double v = a.bias != nullptr || a.group_top == 1 ? c : score;
+      t2 = fmax(t2, fmin(t1, v));
+      t1 = fmax(t1, v);
     }
-  if (a.G > 1) {
+  }
+  if (groups) {
 #pragma unroll 1
     for (int d = a.lanes_per_group >> 1; d >= 1; d >>= 1) {
       const double o1 = __shfl_xor_sync(0xffffffffu, t1, d), o2 = __shfl_xor_sync(0xffffffffu, t2, d);
@@ -181,26 +174,30 @@ __device__ __noinline__ int select_exact(const ScoredArgs& a, const float* row, 
       const double w = __shfl_sync(0xffffffffu, v, o << a.lanes_log2);
       before += w > v || (w == v && o < g);
     }
-    if (before >= a.top_groups) mine = 0;
+    if (before >= a.top_groups) mask = 0u;
   }
-  int id = 0;
+  int id = 0, at = 0;
+  unsigned long long best = 0ull;
+  bool again = true;  // the lane has to look for its best
 #pragma unroll 1
   for (int r = 0; r < a.K; ++r) {
-    unsigned long long best = 0ull;
-    int at = 0;
+    if (again) {
+      best = 0ull;
 #pragma unroll 1
-    for (int i0 = 0; i0 < mine; i0 += kSide)
-#pragma unroll
-      for (int i = i0; i < i0 + kSide; ++i)
-        if (i < mine && key[i] > best) {  // (ascending i: the lower index stays)
+      for (uint32_t m = mask; m != 0u; m &= m - 1u) {
+        const int i = __ffs((int)m) - 1;
+        if (key[i] > best) {  // (ascending i: the lower index stays; no key is zero)
           best = key[i];
           at = i;
         }
+      }
+    }
     const uint32_t hi = (uint32_t)(best >> 32), hi_max = __reduce_max_sync(0xffffffffu, hi);
     const uint32_t lo = hi == hi_max ? (uint32_t)best : 0u, lo_max = __reduce_max_sync(0xffffffffu, lo);
     const int winner = __ffs((int)__ballot_sync(0xffffffffu, hi == hi_max && (uint32_t)best == lo_max)) - 1;
     const int chosen = __shfl_sync(0xffffffffu, first + at, winner);
-    if (lane == winner) key[at] = 0ull;
+    again = lane == winner;
+    if (again) mask &= ~(1u << at);
     if (lane == r) id = chosen;
   }
   return id;
@@ -260,7 +257,8 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
   const float* const row = a.logits + (int64_t)t * a.stride;
   const float kNone = __int_as_float(0xff800000);
   float top = kNone, sum = 1.0f, slack = 0.0f;
-  bool near = false;  // decided again in fp64: near choices, and tokens with a NaN
+  bool near = false;        // two choices are too near to each other
+  bool near_group = false;  // ... or two groups, or there is a NaN: everything is decided again
   uint32_t key[PER];
   float z[PER];
   if (a.softmax) {  // (fmaxf reads a NaN as -inf)
@@ -283,13 +281,13 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const float c = (a.softmax ? z[i] * inverse : fast_sigmoid(l[i])) + bias[i];
-      near = near || ((FULL || i < mine) && !(c + l[i] == c + l[i]));
+      near_group = near_group || ((FULL || i < mine) && !(c + l[i] == c + l[i]));
       key[i] = FULL || i < mine ? sort_key(c) : 0u;
     }
   } else {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      near = near || ((FULL || i < mine) && !(l[i] == l[i]));
+      near_group = near_group || ((FULL || i < mine) && !(l[i] == l[i]));
       key[i] = FULL || i < mine ? sort_key(__fadd_rn(l[i], 0.0f)) : 0u;  // (-0 as +0)
     }
   }
@@ -333,7 +331,7 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
     if (a.bias != nullptr || a.group_top == 2) {  // the border between the groups that stay and the others
       const uint32_t worst = __reduce_min_sync(0xffffffffu, keep && g < a.G ? value : 0xffffffffu);
       const uint32_t best = __reduce_max_sync(0xffffffffu, !keep && g < a.G ? value : 0u);
-      near = near || near_choices(key_value(worst), key_value(best), group_slack);
+      near_group = near_group || near_choices(key_value(worst), key_value(best), group_slack);
     }
     if (!keep) {
 #pragma unroll
@@ -361,8 +359,11 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
     if (lane == a.K - 1) after = next;
     if (lane < a.K && after != 0u) near = near || near_choices(key_value(my_key), key_value(after), slack);
   }
-  near = __any_sync(0xffffffffu, near);
-  if (!near && __any_sync(0xffffffffu, lane < a.K && (my_lanes & (my_lanes - 1u)) != 0u)) {
+  // (with a bias, equal fp32 forms say nothing about the choices)
+  const bool shared = lane < a.K && (my_lanes & (my_lanes - 1u)) != 0u;
+  near_group = __any_sync(0xffffffffu, near_group);
+  near = near_group || __any_sync(0xffffffffu, near || (a.bias != nullptr && shared));
+  if (!near && __any_sync(0xffffffffu, shared)) {
     // equal logits in several lanes (logits that were bf16 have them often): again, the lowest lane alone drops its key
 #pragma unroll
     for (int i = 0; i < PER; ++i) sorted[i] = key[i];
@@ -383,7 +384,15 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
   }
   int id;
   if (near) {
-    id = select_exact<PER>(a, row, lane, first, mine, top);
+    // experts in question: choices that are not clearly below the K-th
+    const float least = key_value(__shfl_sync(0xffffffffu, my_key, a.K - 1));
+    uint32_t mask = 0u;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const bool in = near_group ? FULL || i < mine : key[i] != 0u && (near_choices(least, key_value(key[i]), 2.0f * slack) || key_value(key[i]) >= least);
+      mask |= in ? 1u << i : 0u;
+    }
+    id = select_exact<PER>(a, row, lane, first, mine, top, mask, near_group && a.G > 1);
   } else {
     // equal keys of one lane are taken in the order of their indices
     const int my_lane = __ffs((int)my_lanes) - 1;

@@ -44,6 +44,18 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
       : "memory");
   return done != 0;
 }
+// Has the phase passed?  (mbar_try may hold the thread back for a while where it has not.)
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done != 0;
+}
 // Bounded wait.  Returns false if the CTA is aborting or the time limit ran out.  sleep_ns > 0:
 // the thread sleeps between polls, leaving the issue slots to the warps that have work (the fp8
 // converters share their schedulers with every polling warp).

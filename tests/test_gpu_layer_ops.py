@@ -129,6 +129,16 @@ def test_route_ties_and_near_ties(b, score):
     check_route(b, nudged, (0.75 - s).astype(np.float32), top_k=8, score=score, n_groups=8, top_groups=4, group_top=2)
 
 
+@pytest.mark.parametrize("groups", [(1, 1, 1), (8, 4, 2), (8, 4, 1)])
+def test_route_saturated_scores(b, groups):
+    """Sigmoids that are the same number in fp32 and are not in 64 bits, in ascending order of the index."""
+    e, t = 64, 20
+    rng = np.random.default_rng(8)
+    logits = (16 + np.sort(rng.uniform(0, 4, size=(t, e)), axis=1)).astype(np.float32)
+    for bias in (np.zeros(e, np.float32), np.full(e, 0.25, np.float32)):
+        check_route(b, logits, bias, top_k=8, score=1, n_groups=groups[0], top_groups=groups[1], group_top=groups[2])
+
+
 @pytest.mark.parametrize("score", [0, 1])
 def test_route_non_finite(b, score):
     rng = np.random.default_rng(6)
