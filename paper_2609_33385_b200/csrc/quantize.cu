@@ -1,7 +1,7 @@
 // Activations in front of a product of e4m3 codes: codes and one fp32 scale per row and 128 columns (block_scale.h), of
 // bf16 rows or of silu(gate) * up of rows gate | up, in fp32 from the loads to the codes.
 //
-// Bound by HBM: 2 bytes read (4 with SwiGLU) and 1 written per element.  A half-warp holds a block, eight values (one
+// HBM: 2 bytes read (4 with SwiGLU) and 1 written per element.  A half-warp holds a block, eight values (one
 // 16-byte load) a lane, so that a block's maximum is four shuffles; a warp takes VECS times 256 columns of a row, its
 // loads in flight together: four of them where there are rows enough to fill the GPU (16384 x 4096: 35.2 us, two 37.5), one where
 // there are not (32 x 1024 with SwiGLU 1.9 us, four 2.6).
@@ -38,22 +38,49 @@ quantize_kernel(const uint16_t* __restrict__ x, int64_t x_stride, int64_t pieces
       if (SWIGLU) b[i] = __ldcs(reinterpret_cast<const uint4*>(src + cols + i * 256));
     }
   }
+  if constexpr (SWIGLU) {
 #pragma unroll
-  for (int i = 0; i < VECS; ++i) {
-    float v[8];
-    unpack8(a[i], v);
-    if (SWIGLU) {
-      float u[8];
+    for (int i = 0; i < VECS; ++i) {
+      float v[8], u[8];
+      unpack8(a[i], v);
       unpack8(b[i], u);
       // (the sigmoid's fast exponential and quotient are off by some 2^-21, the code by 2^-4)
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = __fdividef(v[j], 1.0f + __expf(-v[j])) * u[j];
+      const uint32_t amax = amax_half_warp(amax8(v));
+      const int c = c0 + i * 256;
+      if (c < cols) {
+        *reinterpret_cast<uint2*>(codes + row * codes_stride + c) = codes8(v, block_inverse(amax));
+        if ((lane & 15) == 0) scales[row * scales_stride + c / kScaleBlock] = block_scale(amax);
+      }
     }
-    const uint32_t amax = amax_half_warp(amax8(v));
-    const int c = c0 + i * 256;
-    if (c < cols) {
-      *reinterpret_cast<uint2*>(codes + row * codes_stride + c) = codes8(v, block_inverse(amax));
-      if ((lane & 15) == 0) scales[row * scales_stride + c / kScaleBlock] = block_scale(amax);
+  } else {
+    // the blocks' largest magnitudes, two bf16 ones a word: their bits order like the values, and like fp32 ones with 16 zeros behind them
+    uint32_t amax[VECS];
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+      uint32_t big = __vmaxu2(__vmaxu2(a[i].x & 0x7fff7fffu, a[i].y & 0x7fff7fffu), __vmaxu2(a[i].z & 0x7fff7fffu, a[i].w & 0x7fff7fffu));
+#pragma unroll
+      for (int d = 8; d >= 1; d >>= 1) big = __vmaxu2(big, __shfl_xor_sync(0xffffffffu, big, d));
+      amax[i] = max(max(big << 16, big & 0xffff0000u), kAmaxFloor);
+    }
+    // Lane i of a half-warp divides for its block i: quotients for every block in every lane were a third of the kernel's
+    // instructions, which is what it was bound by (16384 x 4096: 35.2 us, now 32.0, as much as a copy).
+    uint32_t mine = amax[0];
+#pragma unroll
+    for (int i = 1; i < VECS; ++i) mine = (lane & (VECS - 1)) == i ? amax[i] : mine;
+    const float my_inverse = block_inverse(mine);
+    {
+      const int block = lane & 15, c = c0 - block * 8 + block * 256;  // (of the half-warp's blocks, 256 columns apart)
+      if (block < VECS && c < cols) scales[row * scales_stride + c / kScaleBlock] = block_scale(mine);
+    }
+#pragma unroll
+    for (int i = 0; i < VECS; ++i) {
+      const float inverse = __shfl_sync(0xffffffffu, my_inverse, (lane & 16) | i);
+      float v[8];
+      unpack8(a[i], v);
+      const int c = c0 + i * 256;
+      if (c < cols) *reinterpret_cast<uint2*>(codes + row * codes_stride + c) = codes8(v, inverse);
     }
   }
 }
