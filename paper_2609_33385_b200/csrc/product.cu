@@ -95,30 +95,45 @@ struct __align__(16) ProductFewCtl {
   int abort;
 };
 
-// Sums of the SPLIT CTAs' partial results ([NT][128] at `ring` in each), and their stores: CTA `rank` has NT / SPLIT columns, a
-// warp one at a time, UNROLL of them requested together (one after the other a column took 170 ns).
-template <int NT, int SPLIT, int UNROLL>
-__device__ __forceinline__ void join_columns(const ProductArgs& p, uint32_t ring, int rank, int warp, int lane, int m0, int n0) {
-  constexpr int kShare = NT / SPLIT, kEpi = few_epi_warps(NT);
-  const int c_end = min(kShare * (rank + 1), p.m - m0);
-  uint32_t base[SPLIT];
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// A tile's columns (rows of A) are joined by the SPLIT CTAs of its cluster, NT / SPLIT each.  Every CTA sends its partial sums to where
+// they are joined - `sums` there: [SPLIT senders][NT / SPLIT columns][128] - as soon as it has them: stores across the cluster are
+// not waited for, loads were, and the CTAs then had to wait for one another a second time before they left (250 x 4096 x
+// 2048: 10.5 us with loads).
+template <int NT, int SPLIT, int COLS>
+__device__ __forceinline__ void send_columns(const float (&acc)[COLS], uint32_t sums, int rank, int col0, int row) {
+  constexpr int kShare = NT / SPLIT, kRun = COLS < kShare ? COLS : kShare;  // columns of the thread that go to one CTA
 #pragma unroll
-  for (int s = 0; s < SPLIT; ++s) base[s] = map_to_cta(ring + (uint32_t)lane * 16u, (uint32_t)s);
-#pragma unroll 1
-  for (int c = kShare * rank + warp; c < c_end; c += kEpi * UNROLL) {
-    float4 part[UNROLL][SPLIT];
+  for (int r = 0; r < COLS; r += kRun) {
+    const int to = (col0 + r) / kShare;
+    const uint32_t at = sums + (uint32_t)((rank * kShare + (col0 + r) % kShare) * 128 + row) * 4u;
+    const uint32_t dst = SPLIT > 1 ? map_to_cta(at, (uint32_t)to) : at;
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      const uint32_t at = (uint32_t)min(c + u * kEpi, NT - 1) * 512u;
-#pragma unroll
-      for (int s = 0; s < SPLIT; ++s)  // (no memory clobber: the loads need not wait for the stores of other columns)
-        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                     : "=f"(part[u][s].x), "=f"(part[u][s].y), "=f"(part[u][s].z), "=f"(part[u][s].w)
-                     : "r"(base[s] + at));
+    for (int c = 0; c < kRun; ++c) {
+      if (SPLIT > 1) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst + (uint32_t)c * 512u), "f"(acc[r + c]) : "memory");
+      else asm volatile("st.shared.f32 [%0], %1;" ::"r"(dst + (uint32_t)c * 512u), "f"(acc[r + c]) : "memory");
     }
+  }
+}
+// The CTA's columns, the senders' parts added in order, a warp one column at a time and four of them requested together.
+template <int NT, int SPLIT>
+__device__ __forceinline__ void join_columns(const ProductArgs& p, const float* sums, int rank, int warp, int lane, int m0, int n0) {
+  constexpr int kShare = NT / SPLIT, kEpi = few_epi_warps(NT), kTogether = SPLIT > 4 ? 2 : 4;
+  const int n_cols = min(kShare, p.m - m0 - kShare * rank);
+#pragma unroll 1
+  for (int c = warp; c < n_cols; c += kEpi * kTogether) {
+    float4 part[kTogether][SPLIT];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      if (c + u * kEpi >= c_end) break;
+    for (int u = 0; u < kTogether; ++u)
+#pragma unroll
+      for (int s = 0; s < SPLIT; ++s)
+        part[u][s] = *reinterpret_cast<const float4*>(sums + (s * kShare + min(c + u * kEpi, kShare - 1)) * 128 + lane * 4);
+#pragma unroll
+    for (int u = 0; u < kTogether; ++u) {
+      if (c + u * kEpi >= n_cols) break;
       float v[4] = {part[u][0].x, part[u][0].y, part[u][0].z, part[u][0].w};
 #pragma unroll
       for (int s = 1; s < SPLIT; ++s) {
@@ -127,18 +142,17 @@ __device__ __forceinline__ void join_columns(const ProductArgs& p, uint32_t ring
         v[2] += part[u][s].z;
         v[3] += part[u][s].w;
       }
-      store_four(p, m0 + c + u * kEpi, n0 + lane * 4, v, p.vec != 0);
+      store_four(p, m0 + kShare * rank + c + u * kEpi, n0 + lane * 4, v, p.vec != 0);
     }
   }
 }
 
-// blockIdx.x: tile of 128 rows of B x the cluster's CTAs, blockIdx.y: tile of NT rows of A.  Dynamic shared memory: control,
-// [k-blocks of the CTA][NT] scales, then on a 1024-byte boundary the ring of `stages` (weight tile, rows of A), which
-// holds the CTA's [NT][128] partial sums in the end.
-template <int NT>
+// blockIdx.x: tile of 128 rows of B x the SPLIT CTAs of a cluster, blockIdx.y: tile of NT rows of A.  Dynamic shared memory: control,
+// [k-blocks of the CTA][NT] scales, then on a 1024-byte boundary the ring of `stages` (weight tile, rows of A), then the sums.
+template <int NT, int SPLIT>
 __global__ void __launch_bounds__((few_epi_warps(NT) + 2) * 32, 1)
 product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a,
-                   const __grid_constant__ ProductArgs p, int stages, int split) {
+                   const __grid_constant__ ProductArgs p, int stages) {
   constexpr int kEpi = few_epi_warps(NT), kProducer = kEpi, kMma = kEpi + 1;
   constexpr int kCols = NT / (kEpi / 4);  // columns of an epilogue warp
   constexpr uint32_t kStage = kWTile + NT * 128;
@@ -146,11 +160,13 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
   ProductFewCtl* const ctl = reinterpret_cast<ProductFewCtl*>(smem_raw);
   float* const s_scale = reinterpret_cast<float*>(smem_raw + sizeof(ProductFewCtl));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = split > 1 ? (int)cluster_cta_rank() : 0;
-  const int n_tile = (int)blockIdx.x / split, n0 = n_tile * 128, m0 = (int)blockIdx.y * NT;
-  const int kb0 = (int)((int64_t)p.k_blocks * rank / split), kb1 = (int)((int64_t)p.k_blocks * (rank + 1) / split);
+  const int rank = SPLIT > 1 ? (int)cluster_cta_rank() : 0;
+  const int n_tile = (int)blockIdx.x / SPLIT, n0 = n_tile * 128, m0 = (int)blockIdx.y * NT;
+  const int kb0 = (int)((int64_t)p.k_blocks * rank / SPLIT), kb1 = (int)((int64_t)p.k_blocks * (rank + 1) / SPLIT);
   const int kbs = kb1 - kb0;
-  const uint32_t ring = (smem_u32(s_scale) + (uint32_t)((p.k_blocks + split - 1) / split) * NT * 4u + 1023u) & ~1023u;
+  const uint32_t smem0 = smem_u32(smem_raw);
+  const uint32_t ring = (smem_u32(s_scale) + (uint32_t)((p.k_blocks + SPLIT - 1) / SPLIT) * NT * 4u + 1023u) & ~1023u;
+  const uint32_t sums = ring + (uint32_t)stages * kStage;
   volatile int* const abort_flag = &ctl->abort;
   const auto load = [&](int i, int stage) {
     const uint32_t bar = smem_u32(&ctl->full[stage]), dst = ring + (uint32_t)stage * kStage;
@@ -159,7 +175,8 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
     tma_load_2d(&map_a, dst + kWTile, bar, (kb0 + i) * 128, m0);
   };
 
-  // Before the CTA's first barrier: the first loads are on their way, tensor memory is taken, the scales are in place.
+  if (SPLIT > 1) cluster_arrive_relaxed();  // "this CTA runs": waited for before the first store into another one
+  // Before the CTA's first barrier the first loads set out and tensor memory is taken.
   if (warp == kProducer) {
     if (lane == 0) {
       asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_b)) : "memory");
@@ -188,15 +205,7 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   } else {
-    // scales of the CTA's k-blocks, those of A times that of B; zero behind the last row
     griddep_wait();
-    for (int i = threadIdx.x; i < kbs * NT; i += kEpi * 32) {
-      const int c = i / kbs, b = i - c * kbs;
-      float s = 0.0f;
-      if (m0 + c < p.m)
-        s = p.a_scale[(int64_t)(m0 + c) * p.a_scale_stride + kb0 + b] * p.b_scale[(int64_t)n_tile * p.b_scale_stride + kb0 + b];
-      s_scale[b * NT + c] = s;
-    }
   }
   tc_fence_before();
   __syncthreads();
@@ -204,7 +213,6 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
   griddep_launch_dependents();
   const uint32_t tmem = ctl->tmem_base;
 
-  float acc[kCols];
   if (warp == kProducer) {
     bool ok = true;
     for (int i = stages; i < kbs && ok; ++i) {
@@ -218,13 +226,16 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
       while (globaltimer() - t0 < 2000000ull) {
       }
     }
+    if (SPLIT > 1) cluster_wait();
   } else if (warp == kMma) {
     const uint64_t w_desc0 = make_smem_desc(ring), x_desc0 = make_smem_desc(ring + kWTile);
     const uint32_t idesc = make_idesc_e4m3(NT);
+    int stage = 0;
+    uint32_t phase = 0;
     for (int i = 0; i < kbs; ++i) {
-      const int stage = i % stages, buf = i % kFewAccs;
-      if (!product_warp_wait(smem_u32(&ctl->acc_empty[buf]), ((uint32_t)(i / kFewAccs) & 1u) ^ 1u, abort_flag)) break;
-      if (!product_warp_wait(smem_u32(&ctl->full[stage]), (uint32_t)(i / stages) & 1u, abort_flag)) break;
+      const int buf = i % kFewAccs;
+      if (i >= kFewAccs && !product_warp_wait(smem_u32(&ctl->acc_empty[buf]), ((uint32_t)(i / kFewAccs) & 1u) ^ 1u, abort_flag)) break;
+      if (!product_warp_wait(smem_u32(&ctl->full[stage]), phase, abort_flag)) break;
       tc_fence_after();
       if (elect_one()) {
         const uint64_t off = (uint64_t)((uint32_t)stage * (kStage >> 4));
@@ -232,14 +243,40 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
         tc_mma_desc<true, false>(d, w_desc0 + off, x_desc0 + off, idesc);
 #pragma unroll
         for (int k = 1; k < 4; ++k) tc_mma_desc<true, true>(d, w_desc0 + off + k * 2, x_desc0 + off + k * 2, idesc);
-        tc_commit(smem_u32(&ctl->empty[stage]));
         tc_commit(smem_u32(&ctl->acc_full[buf]));
+        if (i + stages < kbs) tc_commit(smem_u32(&ctl->empty[stage]));
       }
       __syncwarp();
+      if (++stage == stages) {
+        stage = 0;
+        phase ^= 1u;
+      }
     }
+    asm volatile("bar.sync 2, %0;" ::"n"((kEpi + 1) * 32) : "memory");  // the epilogue warps have read their last columns
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kFewAccs * NT) : "memory");
+    if (SPLIT > 1) cluster_wait();
   } else {
+    // scales of the CTA's k-blocks, those of A times that of B; zero behind the last row
+    for (int i0 = threadIdx.x; i0 < kbs * NT; i0 += kEpi * 32 * 4) {
+      float s[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * kEpi * 32, c = i / kbs, b = i - c * kbs;
+        s[u] = i < kbs * NT && m0 + c < p.m ? __ldg(p.a_scale + (int64_t)(m0 + c) * p.a_scale_stride + kb0 + b) *
+                                                  __ldg(p.b_scale + (int64_t)n_tile * p.b_scale_stride + kb0 + b)
+                                            : 0.0f;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * kEpi * 32, c = i / kbs, b = i - c * kbs;
+        if (i < kbs * NT) s_scale[b * NT + c] = s[u];
+      }
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(kEpi * 32) : "memory");
     const int quarter = warp & 3, c0 = (warp >> 2) * kCols;
     const uint32_t t_row = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c0;
+    float acc[kCols];
 #pragma unroll
     for (int c = 0; c < kCols; ++c) acc[c] = 0.0f;
     bool ok = true;
@@ -271,33 +308,23 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
         }
       }
     }
+    tc_fence_before();
+    asm volatile("bar.arrive 2, %0;" ::"n"((kEpi + 1) * 32) : "memory");
     if (!ok) {
 #pragma unroll
       for (int c = 0; c < kCols; ++c) acc[c] = __int_as_float(0x7fffffff);
     }
+    if (SPLIT > 1) cluster_wait();  // (every CTA runs)
+    send_columns<NT, SPLIT>(acc, sums, rank, c0, quarter * 32 + lane);
   }
-  tc_fence_before();
-  __syncthreads();  // the MMAs have read the ring
-  if (warp == kMma) {
-    tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kFewAccs * NT) : "memory");
+  __syncwarp();
+  if (SPLIT > 1) {
+    cluster_arrive();
+    cluster_wait();  // everything has arrived, and nobody reads or writes another CTA's shared memory from here on
+  } else {
+    __syncthreads();
   }
-  // Every CTA's partial sums go to its own ring; CTA r adds up and stores its share of the columns, a warp one column at a time.
-  // (Stored by the lanes that hold them, 64 columns of two bytes each took longer than the product itself.)
-  if (warp < kEpi) {
-    const uint32_t at = ring + (uint32_t)((warp >> 2) * kCols * 128 + (warp & 3) * 32 + lane) * 4u;
-#pragma unroll
-    for (int c = 0; c < kCols; ++c) asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + (uint32_t)c * 512u), "f"(acc[c]) : "memory");
-  }
-  if (split > 1) cluster_sync_all();
-  else __syncthreads();
-  if (warp < kEpi) {
-    if (split == 1) join_columns<NT, 1, 4>(p, ring, 0, warp, lane, m0, n0);
-    else if (split == 2) join_columns<NT, 2, 4>(p, ring, rank, warp, lane, m0, n0);
-    else if (split == 4) join_columns<NT, 4, 2>(p, ring, rank, warp, lane, m0, n0);
-    else join_columns<NT, 8, 2>(p, ring, rank, warp, lane, m0, n0);
-  }
-  if (split > 1) cluster_sync_all();  // nobody leaves while another CTA may still read its sums
+  if (warp < kEpi) join_columns<NT, SPLIT>(p, reinterpret_cast<const float*>(smem_raw + (sums - smem0)), rank, warp, lane, m0, n0);
 }
 
 // ---- many rows of A: pairs of CTAs -------------------------------------------------------------
@@ -561,22 +588,30 @@ bool output_map(CUtensorMap* m, const ProductArgs& p) {
   return encode_tensor_map(m, 2, p.out, dims, strides, box, false, false, p.out_fp32);
 }
 
+template <int NT, int SPLIT>
+int launch_few_split(cudaStream_t st, const CUtensorMap& map_b, const CUtensorMap& map_a, const ProductArgs& p) {
+  // (per device: the attribute belongs to the kernel of the current context)
+  if (cudaFuncSetAttribute(product_few_kernel<NT, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kProductSmem) != cudaSuccess)
+    return OLED_ERR_CUDA;
+  const int tiles_n = (p.n + 127) / 128, tiles_m = (p.m + NT - 1) / NT, kbs = (p.k_blocks + SPLIT - 1) / SPLIT;
+  constexpr size_t kStage = kWTile + NT * 128;
+  const size_t fixed = sizeof(ProductFewCtl) + (size_t)kbs * NT * 4 + (size_t)NT * 512 + 2048;
+  const int stages = (int)std::min<size_t>({(size_t)kFewStages, (size_t)kbs, (kProductSmem - fixed) / kStage});
+  const cudaError_t err = launch_cluster(product_few_kernel<NT, SPLIT>, dim3((unsigned)(tiles_n * SPLIT), (unsigned)tiles_m),
+                                         dim3((few_epi_warps(NT) + 2) * 32), fixed + stages * kStage, st, SPLIT, map_b, map_a, p, stages);
+  return err == cudaSuccess ? OLED_OK : OLED_ERR_CUDA;
+}
 template <int NT>
 int launch_few(cudaStream_t st, const CUtensorMap& map_b, const CUtensorMap& map_a, const ProductArgs& p) {
-  // (per device: the attribute belongs to the kernel of the current context)
-  if (cudaFuncSetAttribute(product_few_kernel<NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kProductSmem) != cudaSuccess)
-    return OLED_ERR_CUDA;
-  const int tiles_n = (p.n + 127) / 128, tiles_m = (p.m + NT - 1) / NT;
+  const int64_t tiles = (int64_t)((p.n + 127) / 128) * ((p.m + NT - 1) / NT);
   int split = 1;
-  while (split < 8 && 2 * split <= p.k_blocks && (int64_t)tiles_n * tiles_m * split * 2 <= 148) split *= 2;
-  const int kbs = (p.k_blocks + split - 1) / split;
-  constexpr size_t kStage = kWTile + NT * 128;
-  const size_t fixed = sizeof(ProductFewCtl) + (size_t)kbs * NT * 4 + 2048;
-  const int stages = (int)std::min<size_t>({(size_t)kFewStages, (size_t)kbs, (kProductSmem - fixed) / kStage});
-  const size_t smem = fixed + std::max(stages * kStage, (size_t)NT * 512);
-  const cudaError_t err = launch_cluster(product_few_kernel<NT>, dim3((unsigned)(tiles_n * split), (unsigned)tiles_m),
-                                         dim3((few_epi_warps(NT) + 2) * 32), smem, st, split, map_b, map_a, p, stages, split);
-  return err == cudaSuccess ? OLED_OK : OLED_ERR_CUDA;
+  while (split < 8 && 2 * split <= p.k_blocks && tiles * split * 2 <= 148) split *= 2;
+  switch (split) {
+    case 1: return launch_few_split<NT, 1>(st, map_b, map_a, p);
+    case 2: return launch_few_split<NT, 2>(st, map_b, map_a, p);
+    case 4: return launch_few_split<NT, 4>(st, map_b, map_a, p);
+    default: return launch_few_split<NT, 8>(st, map_b, map_a, p);
+  }
 }
 
 int launch_pair(cudaStream_t st, const CUtensorMap& map_b, const CUtensorMap& map_a, const ProductArgs& p) {
