@@ -572,7 +572,6 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
 }
 
 constexpr size_t kProductSmem = 222 * 1024;
-constexpr int kFewRows = 256;
 
 bool byte_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t stride, int box_rows) {
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride};
@@ -604,8 +603,10 @@ int launch_few_split(cudaStream_t st, const CUtensorMap& map_b, const CUtensorMa
 template <int NT>
 int launch_few(cudaStream_t st, const CUtensorMap& map_b, const CUtensorMap& map_a, const ProductArgs& p) {
   const int64_t tiles = (int64_t)((p.n + 127) / 128) * ((p.m + NT - 1) / NT);
-  int split = 1;
-  while (split < 8 && 2 * split <= p.k_blocks && tiles * split * 2 <= 148) split *= 2;
+  // as many CTAs to a tile as run at once: 74 clusters of two, 33 of four, 15 of eight (a GPC has 16 to 20 SMs, and an SM room for
+  // one CTA; 128 x 128 t x 2048: t = 15 6.4 us, t = 16 in eights 10.7, in fours 6.5)
+  int split = tiles <= 15 ? 8 : tiles <= 33 ? 4 : tiles <= 74 ? 2 : 1;
+  while (split > p.k_blocks) split /= 2;
   switch (split) {
     case 1: return launch_few_split<NT, 1>(st, map_b, map_a, p);
     case 2: return launch_few_split<NT, 2>(st, map_b, map_a, p);
@@ -619,7 +620,8 @@ int launch_pair(cudaStream_t st, const CUtensorMap& map_b, const CUtensorMap& ma
     return OLED_ERR_CUDA;
   const int64_t item = p.out_fp32 ? 4 : 2;
   CUtensorMap map_out = map_a;
-  const bool bulk = !off_boundary(p.out, 16) && p.out_stride * item % 16 == 0 && p.out_stride * item < (1ll << 40);
+  // (a bulk store writes whole 16-byte pieces, also of one that ends behind the last column)
+  const bool bulk = !off_boundary(p.out, 16) && p.out_stride * item % 16 == 0 && p.n * item % 16 == 0 && p.out_stride * item < (1ll << 40);
   if (bulk && !output_map(&map_out, p)) return OLED_ERR_CUDA;
   const int tiles = (p.m + kManyRows - 1) / kManyRows * ((p.n + kManyCols - 1) / kManyCols);
   const int pairs = std::min(tiles, 148 / 2);
@@ -668,7 +670,11 @@ int matmul_blocks(const oled_product_shape* shape, const void* a, const float* a
   p.out_fp32 = s.out == OLED_FP32;
   p.vec = !off_boundary(out, 4 * item) && s.out_stride % 4 == 0 && (!add || (!off_boundary(add, 8) && s.add_stride % 4 == 0));
   CUtensorMap map_a, map_b;
-  if (m > kFewRows) {
+  // Many rows go to pairs of CTAs once their tiles fill the GPU.  Tiles of 128 x 128 in one wave are faster (512 x 1024 x 4096: 8.3 us, pairs
+  // 17.0; 1000 x 2048 x 1024: 7.6 / 8.3) up to where they are not split and go through many k-blocks (512 x 4096 x 4096: 19.4 / 18.1),
+  // in two waves slower (640 x 4096 x 2048: 20.8 / 11.6; 160 x 16384 x 1024: 12.9 / 8.4).  Up to 64 rows the weights count alone.
+  const int64_t tiles = (int64_t)((m + 127) / 128) * nb;
+  if (m > 64 && tiles > (kb <= 16 ? 148 : 74)) {
     if (!byte_map(&map_a, a, m, s.k, s.a_stride, 128) || !byte_map(&map_b, b, s.n, s.k, s.b_stride, 128)) return OLED_ERR_CUDA;
     const int rc = launch_pair(st, map_b, map_a, p);
     return cudaGetLastError() == cudaSuccess ? rc : OLED_ERR_CUDA;

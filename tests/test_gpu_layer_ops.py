@@ -410,6 +410,25 @@ def test_product_nan_stays_in_its_row_and_column(b, m):
     assert not bad.any()
 
 
+@pytest.mark.parametrize("m,n,k", [(2100, 1531, 384), (1300, 1536, 2192), (4100, 600, 144), (257, 9600, 2064), (2304, 2048, 1024)])
+def test_product_on_pairs(b, m, n, k):
+    """Shapes that go to pairs of CTAs: ragged rows, columns and k, rows of C on and off 16-byte boundaries."""
+    check_product(b, m, n, k)
+    check_product(b, m, n, k, fp32=True, with_add=True, pad=1)
+    check_product(b, m, n, k, fp32=True)
+    check_product(b, m, n, k, with_add=True, in_place=True, pad=8)
+
+
+def test_product_on_pairs_keeps_nan_in_its_row_and_column(b):
+    a, sa, w, sb = product_inputs(2300, 2048, 256)
+    a[1000, 130], w[300, 40] = 0x7F, 0xFF
+    sa[1400, 1] = float("inf")
+    bad = ~torch.isfinite(run_product(b, a, sa, w, sb, True))
+    assert bool(bad[1000].all()) and bool(bad[1400].all()) and bool(bad[:, 300].all())
+    bad[[1000, 1400]], bad[:, 300] = False, False
+    assert not bool(bad.any())
+
+
 def test_product_scales_of_zero_and_spread(b):
     """Zero scales, and blocks of very different scales: a block counts by its scale alone."""
     a, sa, w, sb = product_inputs(40, 256, 1024)
