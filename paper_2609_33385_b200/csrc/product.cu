@@ -33,7 +33,7 @@ struct ProductArgs {
   const uint16_t* add;
   void* out;
   int64_t a_scale_stride, b_scale_stride, add_stride, out_stride;
-  int m, n, k_blocks, out_fp32, vec;  // vec: see store_four
+  int m, n, k_blocks, out_fp32, vec, vec_add;  // vec: see store_four; vec_add: rows of D on 16-byte boundaries
 };
 
 // Four consecutive columns of a row of C.  vec: rows of C (and of D) start on boundaries of four elements.
@@ -340,6 +340,7 @@ struct __align__(16) ProductManyCtl {
   unsigned long long empty[kManyStages];  // in both
   unsigned long long acc_full[2];         // in both
   unsigned long long acc_empty[2];        // in the first CTA: the epilogue warps of both
+  unsigned long long add_full[kManyEpiWarps];  // a warp's rows of D
   uint32_t tmem_base;
   int abort;
 };
@@ -349,7 +350,8 @@ static_assert(sizeof(ProductManyCtl) <= 1024, "control block");
 // The tiles are dealt out in turn (tile t to pair t mod pairs), along a row of C first (the other way 1 % slower).
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kManyThreads, 1)
 product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_a,
-                    const __grid_constant__ CUtensorMap map_out, const __grid_constant__ ProductArgs p, int bulk_out) {
+                    const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_add,
+                    const __grid_constant__ ProductArgs p, int bulk_out) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   ProductManyCtl* const ctl = reinterpret_cast<ProductManyCtl*>(smem_raw);
   const uint32_t ring = (smem_u32(smem_raw) + sizeof(ProductManyCtl) + 1023u) & ~1023u;
@@ -369,6 +371,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
       mbar_init(smem_u32(&ctl->acc_full[s]), 1);
       mbar_init(smem_u32(&ctl->acc_empty[s]), 2 * kManyEpiWarps);
     }
+    for (int s = 0; s < kManyEpiWarps; ++s) mbar_init(smem_u32(&ctl->add_full[s]), 1);
     ctl->abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -458,10 +461,17 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
     const uint32_t stage_out = ring + kManyStages * kManyStage + (uint32_t)warp * kManyOut;
     bool ok = true, ready = false;
     int buf = 0;
-    uint32_t acc_phase = 0;
+    uint32_t acc_phase = 0, add_phase = 0;
     for (int tile = pair; tile < tiles; tile += n_pairs) {
       const int row = (tile / tiles_n) * kManyRows + (int)rank * 128 + quarter * 32 + lane;
       const int col0 = (tile % tiles_n) * kManyCols + half * 128;
+      if (bulk_out && p.add != nullptr && lane == 0 && ok) {  // the tile's rows of D are fetched into the staging beside its products
+        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        const uint32_t bar = smem_u32(&ctl->add_full[warp]);
+        mbar_expect_tx(bar, kManyOut);
+        tma_load_2d(&map_add, stage_out, bar, col0, row);
+        tma_load_2d(&map_add, stage_out + 4096u, bar, col0 + 64, row);
+      }
       const float* const sa = p.a_scale + (int64_t)min(row, p.m - 1) * p.a_scale_stride;
       const float* const sb = p.b_scale + (int64_t)(min(col0, p.n - 1) / 128) * p.b_scale_stride;
       float acc[128];
@@ -502,11 +512,17 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
 #pragma unroll
         for (int c = 0; c < 128; ++c) acc[c] = __int_as_float(0x7fffffff);
       }
-      if (p.add != nullptr && row < p.m) {
-        const uint16_t* const d = p.add + (int64_t)row * p.add_stride + col0;
+      if (bulk_out && p.add != nullptr) {
+        ok = product_warp_wait(smem_u32(&ctl->add_full[warp]), add_phase, abort_flag) && ok;
+        add_phase ^= 1u;
 #pragma unroll
-        for (int c = 0; c < 128; ++c)
-          if (col0 + c < p.n) acc[c] += __uint_as_float((uint32_t)d[c] << 16);
+        for (int c = 0; c < 128; c += 8) {
+          float w[8];
+          unpack8(lds128(stage_out + (uint32_t)(c / 64) * 4096u + (uint32_t)lane * 128u + (uint32_t)((((c & 63) / 8) ^ (lane & 7)) * 16)), w);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc[c + j] += w[j];
+        }
+        __syncwarp();
       }
       if (bulk_out) {
         // rows of 128 bytes, 16-byte pieces where the 128-byte swizzle wants them; a piece of 64 bf16 or 32 fp32 columns at a time
@@ -550,13 +566,44 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           }
         }
-      } else if (row < p.m) {
+      } else {
+        // rows of C anywhere: 64 fp32 columns at a time through the staging, then row by row, a warp's 32 elements next to each other
+        // (stored by the lanes that hold them, 2352 x 687 x 2768 took 47 us, this way 19)
+        const int row0 = row - lane;
 #pragma unroll
-        for (int c = 0; c < 128; ++c)
-          if (col0 + c < p.n) {
-            if (p.out_fp32) static_cast<float*>(p.out)[(int64_t)row * p.out_stride + col0 + c] = acc[c];
-            else static_cast<uint16_t*>(p.out)[(int64_t)row * p.out_stride + col0 + c] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[c]));
+        for (int round = 0; round < 2; ++round) {
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(stage_out + (uint32_t)(j / 8) * 4096u + (uint32_t)lane * 128u +
+                                                                         (uint32_t)(((j & 7) ^ (lane & 7)) * 16)),
+                         "f"(acc[round * 64 + j * 4]), "f"(acc[round * 64 + j * 4 + 1]), "f"(acc[round * 64 + j * 4 + 2]),
+                         "f"(acc[round * 64 + j * 4 + 3])
+                         : "memory");
+          __syncwarp();
+          const float* const staged = reinterpret_cast<const float*>(smem_raw + (stage_out - smem_u32(smem_raw)));
+#pragma unroll 1
+          for (int i0 = 0; i0 < 64; i0 += 8) {
+            float v[8], d[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              const int r = (i0 + u) >> 1, c = col0 + round * 64 + (u & 1) * 32 + lane;
+              v[u] = staged[(u & 1) * 1024 + r * 32 + ((lane >> 2) ^ (r & 7)) * 4 + (lane & 3)];
+              d[u] = 0.0f;
+              if (p.add != nullptr && row0 + r < p.m && c < p.n)
+                d[u] = __uint_as_float((uint32_t)p.add[(int64_t)(row0 + r) * p.add_stride + c] << 16);
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              const int r = (i0 + u) >> 1, c = col0 + round * 64 + (u & 1) * 32 + lane;
+              if (row0 + r < p.m && c < p.n) {
+                if (p.out_fp32) static_cast<float*>(p.out)[(int64_t)(row0 + r) * p.out_stride + c] = v[u] + d[u];
+                else
+                  static_cast<uint16_t*>(p.out)[(int64_t)(row0 + r) * p.out_stride + c] = __bfloat16_as_ushort(__float2bfloat16_rn(v[u] + d[u]));
+              }
+            }
           }
+        }
       }
     }
     if (bulk_out && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -579,12 +626,12 @@ bool byte_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int6
   return encode_tensor_map(m, 2, base, dims, strides, box, true);
 }
 
-// C in pieces of 32 rows x 128 bytes
-bool output_map(CUtensorMap* m, const ProductArgs& p) {
-  const cuuint64_t item = p.out_fp32 ? 4 : 2;
-  const cuuint64_t dims[2] = {(cuuint64_t)p.n, (cuuint64_t)p.m}, strides[1] = {(cuuint64_t)p.out_stride * item};
+// C or D in pieces of 32 rows x 128 bytes
+bool rows_map(CUtensorMap* m, void* base, const ProductArgs& p, int64_t stride, bool fp32) {
+  const cuuint64_t item = fp32 ? 4 : 2;
+  const cuuint64_t dims[2] = {(cuuint64_t)p.n, (cuuint64_t)p.m}, strides[1] = {(cuuint64_t)stride * item};
   const cuuint32_t box[2] = {(cuuint32_t)(128 / item), 32};
-  return encode_tensor_map(m, 2, p.out, dims, strides, box, false, false, p.out_fp32);
+  return encode_tensor_map(m, 2, base, dims, strides, box, false, false, fp32);
 }
 
 template <int NT, int SPLIT>
@@ -619,13 +666,15 @@ int launch_pair(cudaStream_t st, const CUtensorMap& map_b, const CUtensorMap& ma
   if (cudaFuncSetAttribute(product_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kManySmem) != cudaSuccess)
     return OLED_ERR_CUDA;
   const int64_t item = p.out_fp32 ? 4 : 2;
-  CUtensorMap map_out = map_a;
+  CUtensorMap map_out = map_a, map_add = map_a;
   // (a bulk store writes whole 16-byte pieces, also of one that ends behind the last column)
-  const bool bulk = !off_boundary(p.out, 16) && p.out_stride * item % 16 == 0 && p.n * item % 16 == 0 && p.out_stride * item < (1ll << 40);
-  if (bulk && !output_map(&map_out, p)) return OLED_ERR_CUDA;
+  const bool bulk = !off_boundary(p.out, 16) && p.out_stride * item % 16 == 0 && p.n * item % 16 == 0 && p.out_stride * item < (1ll << 40) &&
+                    (p.add == nullptr || p.vec_add);
+  if (bulk && !rows_map(&map_out, p.out, p, p.out_stride, p.out_fp32)) return OLED_ERR_CUDA;
+  if (bulk && p.add != nullptr && !rows_map(&map_add, const_cast<uint16_t*>(p.add), p, p.add_stride, false)) return OLED_ERR_CUDA;
   const int tiles = (p.m + kManyRows - 1) / kManyRows * ((p.n + kManyCols - 1) / kManyCols);
   const int pairs = std::min(tiles, 148 / 2);
-  const cudaError_t err = launch_pdl(product_pair_kernel, dim3((unsigned)(2 * pairs)), dim3(kManyThreads), kManySmem, st, map_b, map_a, map_out, p,
+  const cudaError_t err = launch_pdl(product_pair_kernel, dim3((unsigned)(2 * pairs)), dim3(kManyThreads), kManySmem, st, map_b, map_a, map_out, map_add, p,
                                      bulk ? 1 : 0);
   return err == cudaSuccess ? OLED_OK : OLED_ERR_CUDA;
 }
@@ -668,6 +717,7 @@ int matmul_blocks(const oled_product_shape* shape, const void* a, const float* a
   p.n = s.n;
   p.k_blocks = kb;
   p.out_fp32 = s.out == OLED_FP32;
+  p.vec_add = !off_boundary(add, 16) && s.add_stride % 8 == 0 && s.add_stride < (1ll << 39);
   p.vec = !off_boundary(out, 4 * item) && s.out_stride % 4 == 0 && (!add || (!off_boundary(add, 8) && s.add_stride % 4 == 0));
   CUtensorMap map_a, map_b;
   // Many rows go to pairs of CTAs once their tiles fill the GPU.  Tiles of 128 x 128 in one wave are faster (512 x 1024 x 4096: 8.3 us, pairs
