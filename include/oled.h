@@ -373,8 +373,8 @@ int oled_route_noalloc(const void* hidden, const void* w_router, const float* bi
  * What an MoE layer of a served model has next to its routed experts.  Each call works on device memory of the
  * current device that the caller owns, is enqueued on cuda_stream (a stream of that device) and needs no context; the library allocates
  * nothing and keeps nothing between calls, so calls may overlap, be captured and be replayed in any order, provided
- * that they write different arrays.  Rows may lie further apart than they are long (strides count elements; what lies
- * between rows is neither read nor written); arrays that a call writes may overlap nothing else that it is given,
+ * that they write different arrays (scratch is one that a call writes).  Rows may lie further apart than they are long (strides count elements, at most 2^36; what lies
+ * between rows is not used and stays as it is); arrays that a call writes may overlap nothing else that it is given,
  * unless said otherwise.  Every argument is checked before anything is launched (INVALID_ARG); no rows at all is no error. */
 #define OLED_BF16 0
 #define OLED_FP32 1
@@ -447,8 +447,8 @@ int oled_quantize_blocks(const void* x, int64_t x_stride, int32_t rows, int32_t 
 /* out[m, n] = sum_k (a[m, k] * a_scale[m, k / 128]) * (b[n, k] * b_scale[n / 128, k / 128]) (+ add[m, n]): the products of a dense
  * expert, of e4m3 codes.  Accumulated in fp32, rounded once.
  *   a: [m, k] codes, b: [n, k] codes; 16-byte aligned rows (strides multiples of 16), k a multiple of 16, at most OLED_MAX_PRODUCT_K.
- *   a_scale fp32 [m, ceil(k / 128)], b_scale fp32 [ceil(n / 128), ceil(k / 128)]; a product of two scales has to be a normal
- *   number.  A code that is NaN makes its row (of a) or column (of b) NaN.
+ *   a_scale fp32 [m, ceil(k / 128)], b_scale fp32 [ceil(n / 128), ceil(k / 128)]; a product of two scales has to be zero or a
+ *   normal number.  A code that is NaN makes its row (of a) or column (of b) NaN.
  *   add: [m, n] bf16 or NULL, may be out itself.  out: [m, n] in `out`'s type.  m at most OLED_MAX_ROUTE_TOKENS (TOO_MANY_TOKENS).
  * Should a device-side wait run out (2 s), the tile's results are NaN. */
 typedef struct {

@@ -293,7 +293,7 @@ norm_odd_kernel(const __grid_constant__ NormArgs a) {
 
 template <typename R>
 cudaError_t launch_norm_kind(cudaStream_t st, const NormArgs& a, bool vec) {
-  const dim3 row((unsigned)a.tokens), rows4((unsigned)((a.tokens + 3) / 4));
+  const dim3 row((unsigned)a.tokens), rows4((unsigned)(((int64_t)a.tokens + 3) / 4));
   if (!vec) {
     if (a.hidden <= 512) return launch_pdl(norm_odd_kernel<R, 128, 4>, row, dim3(128), 0, st, a);
     if (a.hidden <= 2048) return launch_pdl(norm_odd_kernel<R, 256, 8>, row, dim3(256), 0, st, a);
@@ -325,8 +325,9 @@ int norm_residual(const oled_norm_shape* shape, const void* x, const void* y, co
   if (!x || (!y && (post_weight || gate)) || ((h || h_codes) != (pre_weight != nullptr)) || ((h_codes != nullptr) != (h_scales != nullptr)) ||
       (!x_out && !h && !h_codes))
     return OLED_ERR_INVALID_ARG;
-  if (s.x_stride < H || (y && s.y_stride < H) || (gate && s.gate_stride < H) || (x_out && s.x_out_stride < H) ||
-      (h && s.h_stride < H) || (h_codes && (s.codes_stride < H || s.scales_stride < blocks)))
+  if (!stride_ok(s.x_stride, H) || (y && !stride_ok(s.y_stride, H)) || (gate && !stride_ok(s.gate_stride, H)) ||
+      (x_out && !stride_ok(s.x_out_stride, H)) || (h && !stride_ok(s.h_stride, H)) ||
+      (h_codes && (!stride_ok(s.codes_stride, H) || !stride_ok(s.scales_stride, blocks))))
     return OLED_ERR_INVALID_ARG;
   if (off_boundary(x, item) || off_boundary(x_out, item) || off_boundary(y, 2) || off_boundary(post_weight, 2) || off_boundary(gate, 2) ||
       off_boundary(pre_weight, 2) || off_boundary(h, 2) || off_boundary(h_scales, 4))

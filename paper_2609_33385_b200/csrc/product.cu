@@ -668,8 +668,7 @@ int launch_pair(cudaStream_t st, const CUtensorMap& map_b, const CUtensorMap& ma
   const int64_t item = p.out_fp32 ? 4 : 2;
   CUtensorMap map_out = map_a, map_add = map_a;
   // (a bulk store writes whole 16-byte pieces, also of one that ends behind the last column)
-  const bool bulk = !off_boundary(p.out, 16) && p.out_stride * item % 16 == 0 && p.n * item % 16 == 0 && p.out_stride * item < (1ll << 40) &&
-                    (p.add == nullptr || p.vec_add);
+  const bool bulk = !off_boundary(p.out, 16) && p.out_stride * item % 16 == 0 && p.n * item % 16 == 0 && (p.add == nullptr || p.vec_add);
   if (bulk && !rows_map(&map_out, p.out, p, p.out_stride, p.out_fp32)) return OLED_ERR_CUDA;
   if (bulk && p.add != nullptr && !rows_map(&map_add, const_cast<uint16_t*>(p.add), p, p.add_stride, false)) return OLED_ERR_CUDA;
   const int tiles = (p.m + kManyRows - 1) / kManyRows * ((p.n + kManyCols - 1) / kManyCols);
@@ -688,8 +687,8 @@ int matmul_blocks(const oled_product_shape* shape, const void* a, const float* a
   if (s.n <= 0 || s.n > (1 << 20) || s.k <= 0 || s.k > OLED_MAX_PRODUCT_K || s.k % 16 != 0 || (s.out != OLED_BF16 && s.out != OLED_FP32) || m < 0)
     return OLED_ERR_INVALID_ARG;
   const int kb = (s.k + 127) / 128, nb = (s.n + 127) / 128;
-  if (s.a_stride < s.k || s.a_stride % 16 != 0 || s.b_stride < s.k || s.b_stride % 16 != 0 || s.a_scale_stride < kb || s.b_scale_stride < kb ||
-      s.out_stride < s.n || (add && s.add_stride < s.n) || s.a_stride >= (1ll << 40) || s.b_stride >= (1ll << 40))
+  if (!stride_ok(s.a_stride, s.k) || s.a_stride % 16 != 0 || !stride_ok(s.b_stride, s.k) || s.b_stride % 16 != 0 ||
+      !stride_ok(s.a_scale_stride, kb) || !stride_ok(s.b_scale_stride, kb) || !stride_ok(s.out_stride, s.n) || (add && !stride_ok(s.add_stride, s.n)))
     return OLED_ERR_INVALID_ARG;
   if (m > OLED_MAX_ROUTE_TOKENS) return OLED_ERR_TOO_MANY_TOKENS;
   if (m == 0) return OLED_OK;
@@ -717,7 +716,7 @@ int matmul_blocks(const oled_product_shape* shape, const void* a, const float* a
   p.n = s.n;
   p.k_blocks = kb;
   p.out_fp32 = s.out == OLED_FP32;
-  p.vec_add = !off_boundary(add, 16) && s.add_stride % 8 == 0 && s.add_stride < (1ll << 39);
+  p.vec_add = !off_boundary(add, 16) && s.add_stride % 8 == 0;
   p.vec = !off_boundary(out, 4 * item) && s.out_stride % 4 == 0 && (!add || (!off_boundary(add, 8) && s.add_stride % 4 == 0));
   CUtensorMap map_a, map_b;
   // Many rows go to pairs of CTAs once their tiles fill the GPU.  Tiles of 128 x 128 in one wave are faster (512 x 1024 x 4096: 8.3 us, pairs

@@ -106,8 +106,8 @@ extern "C" int oled_quantize_blocks(const void* x, int64_t x_stride, int32_t row
   using namespace oled;
   const int64_t width = swiglu ? 2 * (int64_t)cols : (int64_t)cols;
   const int blocks = cols > 0 ? (cols + kScaleBlock - 1) / kScaleBlock : 0;
-  if (rows < 0 || cols <= 0 || cols % 16 != 0 || cols > OLED_MAX_PRODUCT_K || (swiglu != 0 && swiglu != 1) || x_stride < width ||
-      x_stride % 8 != 0 || codes_stride < cols || codes_stride % 16 != 0 || scales_stride < blocks)
+  if (rows < 0 || cols <= 0 || cols % 16 != 0 || cols > OLED_MAX_PRODUCT_K || (swiglu != 0 && swiglu != 1) || !stride_ok(x_stride, width) ||
+      x_stride % 8 != 0 || !stride_ok(codes_stride, cols) || codes_stride % 16 != 0 || !stride_ok(scales_stride, blocks))
     return OLED_ERR_INVALID_ARG;
   if (rows == 0) return OLED_OK;
   if (!x || !codes || !scales || off_boundary(x, 16) || off_boundary(codes, 16) || off_boundary(scales, 4))

@@ -775,7 +775,7 @@ extern "C" int oled_route_scored(const oled_routing* routing, const float* logit
                                  int32_t n_tokens, void* cuda_stream, int32_t* ids, float* gate, int32_t* counts, int32_t* offsets,
                                  int32_t* perm, void* scratch, size_t scratch_bytes) {
   using namespace oled;
-  if (!routing_ok(routing) || n_tokens < 0 || logits_stride < routing->n_experts) return OLED_ERR_INVALID_ARG;
+  if (!routing_ok(routing) || n_tokens < 0 || !stride_ok(logits_stride, routing->n_experts)) return OLED_ERR_INVALID_ARG;
   if (n_tokens > OLED_MAX_ROUTE_TOKENS) return OLED_ERR_TOO_MANY_TOKENS;
   const bool order = counts != nullptr;
   if (order != (offsets != nullptr) || (n_tokens > 0 && order != (perm != nullptr))) return OLED_ERR_INVALID_ARG;

@@ -7,6 +7,10 @@ namespace oled {
 
 inline bool off_boundary(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
+// No array's rows are further apart than this (elements): products of strides and rows stay in 64 bits.
+constexpr int64_t kMaxStride = 1ll << 36;
+inline bool stride_ok(int64_t stride, int64_t width) { return stride >= width && stride <= kMaxStride; }
+
 // `rows` rows of `width` bytes, `stride` bytes apart.
 struct RowRange {
   const void* p;

@@ -398,6 +398,40 @@ def test_product_larger(b, m, n, k):
     check_product(b, m, n, k, with_add=True, in_place=True, pad=2)
 
 
+@pytest.mark.parametrize("m,n", [(128, 5000), (64, 9600), (9, 10000)])
+def test_product_long_k_without_many_ctas_to_a_tile(b, m, n):
+    check_product(b, m, n, 16384)
+
+
+def test_offsets_past_32_bits(b):
+    """Arrays of more than 2^32 elements: the last rows are those of a small call, the ones in front of them stay zeros."""
+    r, k = 265000, 16384                                  # 4.3e9 elements
+    last = torch.randn(3, k, device=DEV).to(torch.bfloat16)
+    x = torch.zeros((r, k), dtype=torch.bfloat16, device=DEV)
+    x[-3:] = last
+    codes, scales = torch.full((r, k), 1, dtype=torch.uint8, device=DEV), torch.empty((r, k // 128), device=DEV)
+    c1, s1 = torch.empty((3, k), dtype=torch.uint8, device=DEV), torch.empty((3, k // 128), device=DEV)
+    ok(b, b.quantize_blocks(ptr(x), k, r, k, 0, stream(), ptr(codes), k, ptr(scales), k // 128))
+    ok(b, b.quantize_blocks(ptr(last), k, 3, k, 0, stream(), ptr(c1), k, ptr(s1), k // 128))
+    assert torch.equal(codes[-3:], c1) and torch.equal(scales[-3:], s1) and not bool(codes[:-3].any())
+    w = torch.ones(k, dtype=torch.bfloat16, device=DEV)
+    shape = b.NormShape(hidden=k, residual=0, gate_tokens=0, eps=1e-6, residual_scale=1.0, x_stride=k, y_stride=k, gate_stride=k, x_out_stride=k, h_stride=k,
+                        codes_stride=k, scales_stride=k // 128)
+    h1 = torch.empty_like(last)
+    ok(b, b.norm_residual(shape, ptr(last), None, None, None, ptr(w), 3, stream(), None, ptr(h1), None, None))
+    ok(b, b.norm_residual(shape, ptr(x), None, None, None, ptr(w), r, stream(), None, ptr(x), None, None))
+    assert torch.equal(x[-3:].view(torch.int16), h1.view(torch.int16)) and not bool(x[:-3].any())
+    del x, codes, scales
+    m, n, kk = 70000, 65536, 16                           # 4.6e9 results
+    a, wt = torch.zeros((m, kk), dtype=torch.uint8, device=DEV), torch.full((n, kk), 0x38, dtype=torch.uint8, device=DEV)
+    a[-1], a[1] = 0x38, 0x40                              # 1.0, 2.0
+    sa, sb = torch.ones((m, 1), device=DEV), torch.ones((n // 128, 1), device=DEV)
+    out = torch.empty((m, n), dtype=torch.bfloat16, device=DEV)
+    ps = b.ProductShape(n=n, k=kk, out=0, a_stride=kk, a_scale_stride=1, b_stride=kk, b_scale_stride=1, add_stride=0, out_stride=n)
+    ok(b, b.matmul_blocks(ps, ptr(a), ptr(sa), ptr(wt), ptr(sb), None, m, stream(), ptr(out)))
+    assert bool((out[-1] == 16).all()) and bool((out[1] == 32).all()) and not bool(out[2:-1].any()) and not bool(out[0].any())
+
+
 @pytest.mark.parametrize("m", [3, 200, 1200])
 def test_product_nan_stays_in_its_row_and_column(b, m):
     a, sa, w, sb = product_inputs(m, 512, 512)
@@ -410,7 +444,7 @@ def test_product_nan_stays_in_its_row_and_column(b, m):
     assert not bad.any()
 
 
-@pytest.mark.parametrize("m,n,k", [(2100, 1531, 384), (1300, 1536, 2192), (4100, 600, 144), (257, 9600, 2064), (2304, 2048, 1024)])
+@pytest.mark.parametrize("m,n,k", [(2100, 1531, 384), (1300, 1536, 2192), (4100, 600, 144), (257, 9600, 2064), (2304, 2048, 1024), (5000, 1024, 128)])
 def test_product_on_pairs(b, m, n, k):
     """Shapes that go to pairs of CTAs: ragged rows, columns and k, rows of C on and off 16-byte boundaries."""
     check_product(b, m, n, k)

@@ -107,7 +107,7 @@ def test_route_refuses_arguments(b):
     big = dict(n=1000, scratch=ptr(6))                     # 8000 assignments: sorted through scratch
     need = b.route_scored_scratch(_routing(b), 1000)
     assert need > 0 and b.route_scored_scratch(_routing(b), 512) == 0
-    for kw in (dict(r=None), dict(n=-1), dict(stride=63), dict(logits=None), dict(ids=None), dict(gate=None), dict(counts=None),
+    for kw in (dict(r=None), dict(n=-1), dict(stride=63), dict(stride=(1 << 36) + 1), dict(logits=None), dict(ids=None), dict(gate=None), dict(counts=None),
                dict(offsets=None), dict(perm=None), dict(logits=ptr(0, 2)), dict(ids=ptr(1, 1)), dict(gate=ptr(2, 2)),
                dict(bias=ptr(7, 2)), dict(counts=ptr(3, 2)), dict(offsets=ptr(4, 1)), dict(perm=ptr(5, 3)), dict(ids=ptr(0, 16)),
                dict(gate=ptr(1, 64)), dict(perm=ptr(2)), dict(bias=ptr(3)), dict(big, scratch=None, bytes=need),
@@ -130,7 +130,7 @@ def _norm(b, shape=None, **kw):
 @pytest.mark.parametrize("shape", [
     dict(hidden=0), dict(hidden=16385), dict(residual=2), dict(gate_tokens=-1), dict(eps=0.0), dict(eps=-1.0), dict(eps=math.nan),
     dict(eps=math.inf), dict(residual_scale=math.nan), dict(x_stride=255), dict(y_stride=255), dict(gate_stride=0), dict(x_out_stride=1),
-    dict(h_stride=255), dict(codes_stride=255), dict(scales_stride=1)])
+    dict(h_stride=255), dict(codes_stride=255), dict(scales_stride=1), dict(x_stride=1 << 60), dict(scales_stride=1 << 37)])
 def test_norm_refuses_shape(b, shape):
     assert _norm(b, shape) == b.ERR_INVALID_ARG
 
@@ -156,7 +156,7 @@ def test_quantize_refuses(b):
         a.update(kw)
         return b.quantize_blocks(a["x"], a["xs"], a["rows"], a["cols"], a["sw"], 0, a["codes"], a["cs"], a["scales"], a["ss"])
     for kw in (dict(rows=-1), dict(cols=0), dict(cols=264), dict(cols=16400, xs=16400, cs=16400, ss=200), dict(sw=2), dict(xs=248),
-               dict(xs=257), dict(sw=1), dict(cs=240), dict(cs=264), dict(ss=1), dict(x=None), dict(codes=None), dict(scales=None),
+               dict(xs=257), dict(xs=1 << 40), dict(sw=1), dict(cs=240), dict(cs=264), dict(ss=1), dict(x=None), dict(codes=None), dict(scales=None),
                dict(x=ptr(0, 8)), dict(codes=ptr(1, 8)), dict(scales=ptr(2, 2)), dict(codes=ptr(0)), dict(scales=ptr(0, 64)),
                dict(scales=ptr(1, 64))):
         assert q(**kw) == b.ERR_INVALID_ARG, kw
@@ -177,7 +177,7 @@ def test_matmul_refuses(b):
                dict(out_stride=255), dict(add=ptr(5), add_stride=255), dict(a=None), dict(sa=None), dict(b=None), dict(sb=None), dict(out=None),
                dict(a=ptr(0, 8)), dict(b=ptr(2, 8)), dict(sa=ptr(1, 2)), dict(sb=ptr(3, 2)), dict(add=ptr(5, 1)), dict(out=ptr(4, 1)),
                dict(type=1, out=ptr(4, 2)), dict(out=ptr(0)), dict(out=ptr(1)), dict(out=ptr(2)), dict(out=ptr(3)), dict(add=ptr(4, 64)),
-               dict(type=1, add=ptr(4)), dict(a_stride=1 << 40)):
+               dict(type=1, add=ptr(4)), dict(a_stride=1 << 40), dict(out_stride=1 << 62)):
         assert mm(**kw) == b.ERR_INVALID_ARG, kw
     assert b.matmul_blocks(None, ptr(0), ptr(1), ptr(2), ptr(3), None, 4, 0, ptr(4)) == b.ERR_INVALID_ARG
     assert mm(m=b.MAX_ROUTE_TOKENS + 1) == b.ERR_TOO_MANY_TOKENS
