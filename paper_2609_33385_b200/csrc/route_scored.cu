@@ -319,19 +319,28 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
       t1 += t2;
       group_slack *= 2.0f;
     }
+    // rounds over the groups: the lanes of the largest value are kept and drop out
     const int g = lane >> a.lanes_log2;
-    const uint32_t value = order_key(topk_value(t1));
-    int before = 0;
-#pragma unroll 4
-    for (int o = 0; o < a.G; ++o) {
-      const uint32_t v = __shfl_sync(0xffffffffu, value, o << a.lanes_log2);
-      before += v > value - (o < g ? 1u : 0u);  // (an equal value precedes if its group is lower; no key is zero)
+    const uint32_t value = g < a.G ? order_key(topk_value(t1)) : 0u;
+    uint32_t left = value, last = 0u;
+    for (int r = 0; r < a.top_groups; ++r) {
+      last = __reduce_max_sync(0xffffffffu, left);
+      left = left == last ? 0u : left;
     }
-    const bool keep = before < a.top_groups;
+    const uint32_t next = __reduce_max_sync(0xffffffffu, left);
+    bool keep = value != 0u && left == 0u;
     if (a.bias != nullptr || a.group_top == 2) {  // the border between the groups that stay and the others
-      const uint32_t worst = __reduce_min_sync(0xffffffffu, keep && g < a.G ? value : 0xffffffffu);
-      const uint32_t best = __reduce_max_sync(0xffffffffu, !keep && g < a.G ? value : 0u);
-      near_group = near_group || near_choices(key_value(worst), key_value(best), group_slack);
+      near_group = near_group || next == 0u || near_choices(key_value(last), key_value(next), group_slack);
+    }
+    if (__popc(__ballot_sync(0xffffffffu, keep)) != a.top_groups << a.lanes_log2) {  // equal values: the lower groups
+      near_group = near_group || a.bias != nullptr || a.group_top == 2;               // (fp32 forms: decided again)
+      int before = 0;
+#pragma unroll 1
+      for (int o = 0; o < a.G; ++o) {
+        const uint32_t v = __shfl_sync(0xffffffffu, value, o << a.lanes_log2);
+        before += v > value - (o < g ? 1u : 0u);  // (no key is zero)
+      }
+      keep = g < a.G && before < a.top_groups;
     }
     if (!keep) {
 #pragma unroll
@@ -394,26 +403,25 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
     }
     id = select_exact<PER>(a, row, lane, first, mine, top, mask, near_group && a.G > 1);
   } else {
-    // equal keys of one lane are taken in the order of their indices
-    const int my_lane = __ffs((int)my_lanes) - 1;
-    int skip = 0;
-    {
-      const uint32_t before = __shfl_up_sync(0xffffffffu, my_key, 1);
-      if (__any_sync(0xffffffffu, lane > 0 && lane < a.K && before == my_key)) {
-        const uint32_t same = __match_any_sync(0xffffffffu, my_key) & __match_any_sync(0xffffffffu, my_lane);
-        skip = __popc(same & ((1u << lane) - 1u));
-      }
-    }
+    const int my_lane = (__ffs((int)my_lanes) - 1) & 31;
     int at = 0;
+    const uint32_t before = __shfl_up_sync(0xffffffffu, my_key, 1);
+    if (!__any_sync(0xffffffffu, lane > 0 && lane < a.K && before == my_key)) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const uint32_t k = __shfl_sync(0xffffffffu, key[i], my_lane & 31);
-      if (k == my_key) {
-        if (skip == 0) at = i;
-        --skip;
+      for (int i = 1; i < PER; ++i) at = __shfl_sync(0xffffffffu, key[i], my_lane) == my_key ? i : at;
+    } else {  // equal keys of one lane are taken in the order of their indices
+      const uint32_t same = __match_any_sync(0xffffffffu, my_key) & __match_any_sync(0xffffffffu, my_lane);
+      int skip = __popc(same & ((1u << lane) - 1u));
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const uint32_t k = __shfl_sync(0xffffffffu, key[i], my_lane);
+        if (k == my_key) {
+          if (skip == 0) at = i;
+          --skip;
+        }
       }
     }
-    id = __shfl_sync(0xffffffffu, first, my_lane & 31) + at;
+    id = __shfl_sync(0xffffffffu, first, my_lane) + at;
   }
   // the chosen experts' weights (the quotients are off by two units in the last place at most)
   float s = 0.0f;

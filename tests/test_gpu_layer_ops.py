@@ -139,6 +139,20 @@ def test_route_saturated_scores(b, groups):
         check_route(b, logits, bias, top_k=8, score=1, n_groups=groups[0], top_groups=groups[1], group_top=groups[2])
 
 
+def test_route_groups_of_equal_fp32_value(b):
+    """Two groups far above the others, equal in fp32 and told apart in 64 bits by their index's opposite: one may stay."""
+    e, t = 64, 8
+    logits = np.full((t, e), -3.0, np.float32)
+    for i in range(t):
+        lo_g, hi_g = i, (i + 3) % 8
+        logits[i, lo_g * 8:lo_g * 8 + 2] = 18.0
+        logits[i, hi_g * 8:hi_g * 8 + 2] = np.nextafter(np.float32(18.0), np.float32(19.0))
+    for bias in (None, np.zeros(e, np.float32)):
+        for top_groups in (1, 2, 3):
+            for group_top in (1, 2):
+                check_route(b, logits, bias, top_k=6, score=1, n_groups=8, top_groups=top_groups, group_top=group_top)
+
+
 @pytest.mark.parametrize("score", [0, 1])
 def test_route_non_finite(b, score):
     rng = np.random.default_rng(6)
