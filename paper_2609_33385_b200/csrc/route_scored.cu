@@ -10,13 +10,15 @@
 //
 // The ids are those of the formulas in exact arithmetic as far as 64 bits tell: choices are compared in fp32 first, and a
 // token two of whose compared values lie within the fp32 forms' error (near_choices() below) is decided again in fp64 by
-// the same warp.  That is a few tokens in a thousand with a bias, none without one (logits are compared as they are).
+// the same warp.  That is one token in about two thousand with a bias (256 experts in groups), none without one (logits are
+// compared as they are).
 //
 // A warp per token.  Its lanes are dealt to the groups (32 / G each, G rounded up to a power of two), a lane's experts are
 // consecutive, so that lower lanes hold lower experts and a group never shares a lane with another.  Every lane
 // sorts its keys once (a network of maxima and minima in registers); then each of the top_k rounds is one warp maximum
 // over the lanes' heads, a vote for the lowest lane that has it, and a shift in that lane.
-// Bound by the instructions of a token; the logits' bytes would take a third of the time.
+// Bound by the instructions of a token, 685 a warp at 256 experts in groups (32768 tokens: 45 us, 40 of them this kernel's with its issue
+// slots 66 % full; the bytes would take 6).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
