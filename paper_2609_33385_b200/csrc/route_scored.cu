@@ -54,9 +54,6 @@ struct ScoredArgs {
   const float* conf;
 };
 
-__device__ __forceinline__ float key_value(uint32_t key) {
-  return __uint_as_float((key & 0x80000000u) ? key ^ 0x80000000u : ~key);
-}
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
   for (int d = 16; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
@@ -68,21 +65,26 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 __device__ __forceinline__ float no_nan(float v) { return v == v ? v : __int_as_float(0xff800000); }
-// Descending order of N keys in registers.
+// The warp's largest value (no NaN among them).
+__device__ __forceinline__ float reduce_max(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+// Descending order of N values in registers (Batcher's odd-even merges: 19 exchanges for eight values).
 template <int N>
-__device__ __forceinline__ void sort_desc(uint32_t (&k)[N]) {
+__device__ __forceinline__ void sort_desc(float (&k)[N]) {
 #pragma unroll
-  for (int size = 2; size <= N; size <<= 1)
+  for (int p = 1; p < N; p <<= 1)
 #pragma unroll
-    for (int step = size >> 1; step >= 1; step >>= 1)
+    for (int d = p; d >= 1; d >>= 1)
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int j = i ^ step;
-        if (j > i) {
-          const uint32_t hi = max(k[i], k[j]), lo = min(k[i], k[j]);
-          const bool down = (i & size) == 0 || size == N;
-          k[i] = down ? hi : lo;
-          k[j] = down ? lo : hi;
+        const int at = i - d % p;  // pairs i, i + d lie in stretches of 2 d from d % p on, in their first halves
+        if (at >= 0 && at % (2 * d) < d && i + d < N && i / (2 * p) == (i + d) / (2 * p)) {
+          const float hi = fmaxf(k[i], k[i + d]), lo = fminf(k[i], k[i + d]);
+          k[i] = hi;
+          k[i + d] = lo;
         }
       }
 }
@@ -125,34 +127,115 @@ __device__ __forceinline__ double reciprocal_double(double x) {
   return y;
 }
 
+// The softmax's sum of a token in fp64.
+__device__ __forceinline__ double sum_exact(const float* row, int first, int mine, float top) {
+  double sum = 0.0;
+#pragma unroll 1
+  for (int i = 0; i < mine; ++i) {
+    const float l = no_nan(row[first + i]);
+    sum += exp_double(l == top ? 0.0 : (double)l - (double)top);
+  }
+  for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  return sum;
+}
+// An expert's choice in fp64 (no NaN: -inf), and its score.
+__device__ __forceinline__ double choice_exact(const ScoredArgs& a, const float* row, int e, float top, double sum, double& score) {
+  const float l = row[e], x = no_nan(l);
+  const double ex = exp_double(a.softmax ? (x == top ? 0.0 : (double)x - (double)top) : -(double)x);
+  score = (a.softmax ? ex : 1.0) * reciprocal_double(a.softmax ? sum : 1.0 + ex);
+  const double c = a.bias == nullptr ? (double)l : score + (double)a.bias[e];
+  return l == l && c == c ? c : -INFINITY;
+}
+// Deals the experts of the lanes' masks to the lanes, one each; their number (above 32: none dealt).
+template <int PER>
+__device__ __forceinline__ int deal(uint32_t mask, int lane, int first, int32_t* s_experts, int& expert) {
+  int n = 0;
+  __syncwarp();
+#pragma unroll 1
+  for (int i = 0; i < PER; ++i) {
+    const bool in = (mask >> i) & 1u;
+    const uint32_t lanes = __ballot_sync(0xffffffffu, in);
+    const int at = n + __popc(lanes & ((1u << lane) - 1u));
+    if (in && at < 32) s_experts[at] = first + i;
+    n += __popc(lanes);
+  }
+  __syncwarp();
+  expert = lane < n ? s_experts[lane] : 0;
+  return n;
+}
+
+// Which groups stay, where the border between them lies between values that are too near to each other; sure: the lane's group stays in any
+// case, question: it may (mask: those of its experts that can count for its value).  None of the values is NaN or -inf.
+// False in `decided`: too many experts.
+template <int PER>
+__device__ __noinline__ bool groups_exact(const ScoredArgs& a, const float* row, int lane, int first, int mine, float top, bool sure, bool question,
+                                          uint32_t mask, bool& decided) {
+  __shared__ int32_t s_experts[kScoredWarps][32];
+  int expert;
+  const int n = deal<PER>(mask, lane, first, s_experts[(threadIdx.x >> 5) % kScoredWarps], expert);
+  decided = n <= 32;
+  if (!decided) return false;
+  const double sum = a.softmax ? sum_exact(row, first, mine, top) : 1.0;
+  double value, score;
+  value = choice_exact(a, row, expert, top, sum, score);
+  if (a.bias == nullptr && a.group_top == 2) value = score;
+  const int group = expert / a.group_size, g = lane >> a.lanes_log2;
+  double t1 = -INFINITY, t2 = -INFINITY;
+#pragma unroll 4
+  for (int o = 0; o < n; ++o) {
+    const double v = __shfl_sync(0xffffffffu, value, o);
+    if (__shfl_sync(0xffffffffu, group, o) == g) {
+      t2 = fmax(t2, fmin(t1, v));
+      t1 = fmax(t1, v);
+    }
+  }
+  const double v = a.group_top == 1 ? t1 : t1 + t2;
+  const uint32_t asked = __ballot_sync(0xffffffffu, question);
+  const int places = a.top_groups - (__popc(__ballot_sync(0xffffffffu, sure)) >> a.lanes_log2);
+  int before = 0;
+#pragma unroll 1
+  for (int o = 0; o < a.G; ++o) {
+    const double w = __shfl_sync(0xffffffffu, v, o << a.lanes_log2);
+    before += ((asked >> (o << a.lanes_log2)) & 1u) && (w > v || (w == v && o < g));
+  }
+  return sure || (question && before < places);
+}
+
 // The choice of one token in fp64, by the warp that holds its logits: lane r < K ends with the id of rank r.  mask: the lane's experts
 // that can be among the K.  groups: the groups are chosen again too (all experts are in the masks then).  Scores below exp(-708)
 // count as that.  Few tokens come here, but a CTA waits for the last of its own; what they cost is fp64 latency, so only those
-// experts are computed that the fp32 forms leave in question (with all of them a token took 5.5 us).
+// experts are computed that the fp32 forms leave in question, a lane each where there are lanes for them (lanes with two or three of them
+// in turn, and rounds to order them: 250 tokens with one such 8.4 us, this way WHAT; with all experts a token took 5.5 us).
 template <int PER>
 __device__ __noinline__ int select_exact(const ScoredArgs& a, const float* row, int lane, int first, int mine, float top, uint32_t mask,
                                          bool groups) {
+  __shared__ int32_t s_experts[kScoredWarps][32];
+  int32_t* const experts = s_experts[(threadIdx.x >> 5) % kScoredWarps];
   const double kNone = -INFINITY;
   unsigned long long key[PER];  // of the choices (in local memory: registers count for the whole kernel)
-  double sum = 1.0;
-  if (a.softmax) {
-    sum = 0.0;
-#pragma unroll 1
-    for (int i = 0; i < mine; ++i) {
-      const float l = no_nan(row[first + i]);
-      sum += exp_double(l == top ? 0.0 : (double)l - (double)top);
+  const double sum = a.softmax ? sum_exact(row, first, mine, top) : 1.0;
+  double score;
+  int expert;
+  const int n = groups ? 33 : deal<PER>(mask, lane, first, experts, expert);
+  if (n <= 32) {
+    const double c = choice_exact(a, row, expert, top, sum, score);
+    int before = 0;
+#pragma unroll 4
+    for (int o = 0; o < n; ++o) {
+      const double v = __shfl_sync(0xffffffffu, c, o);
+      const int e = __shfl_sync(0xffffffffu, expert, o);
+      before += v > c || (v == c && e < expert);
     }
-    for (int d = 16; d >= 1; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    __syncwarp();
+    if (lane < n && before < a.K) experts[before] = expert;
+    __syncwarp();
+    return lane < a.K ? experts[lane] : 0;
   }
   double t1 = kNone, t2 = kNone;
 #pragma unroll 1
   for (uint32_t m = mask; m != 0u; m &= m - 1u) {
     const int i = __ffs((int)m) - 1;
-    const float l = row[first + i], x = no_nan(l);
-    const double e = exp_double(a.softmax ? (x == top ? 0.0 : (double)x - (double)top) : -(double)x);
-    const double score = (a.softmax ? e : 1.0) * reciprocal_double(a.softmax ? sum : 1.0 + e);
-    double c = a.bias == nullptr ? (double)l : score + (double)a.bias[first + i];
-    if (!(l == l) || !(c == c)) c = kNone;
+    const double c = choice_exact(a, row, first + i, top, sum, score);
     key[i] = order_key64(c + 0.0);
     if (groups) {
       const double v = a.bias != nullptr || a.group_top == 1 ? c : score;
@@ -225,11 +308,6 @@ __device__ __forceinline__ float fast_reciprocal(float x) {
   return r;
 }
 __device__ __forceinline__ float fast_sigmoid(float l) { return fast_reciprocal(1.0f + fast_exp(-l)); }
-// order_key() in two instructions; a NaN's is above that of +inf or below that of -inf.
-__device__ __forceinline__ uint32_t sort_key(float v) {
-  const uint32_t bits = __float_as_uint(v);
-  return bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u);
-}
 
 // A token's logits, as its lanes hold them.  PER: experts a lane has room for.  FULL: every lane has that many.
 template <int PER, bool FULL>
@@ -260,8 +338,8 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
   const float kNone = __int_as_float(0xff800000);
   float top = kNone, sum = 1.0f, slack = 0.0f;
   bool near = false;        // two choices are too near to each other
-  bool near_group = false;  // ... or two groups, or there is a NaN: everything is decided again
-  uint32_t key[PER];
+  bool near_group = false;  // ... or two groups, or there is a NaN, or too little that is not -inf: everything is decided again
+  float key[PER];           // what is compared (-inf: there is no such expert, or as good as none)
   float z[PER];
   if (a.softmax) {  // (fmaxf reads a NaN as -inf)
 #pragma unroll
@@ -283,29 +361,35 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const float c = (a.softmax ? z[i] * inverse : fast_sigmoid(l[i])) + bias[i];
-      near_group = near_group || ((FULL || i < mine) && !(c + l[i] == c + l[i]));
-      key[i] = FULL || i < mine ? sort_key(c) : 0u;
+      near_group = near_group || ((FULL || i < mine) && !(c == c));
+      key[i] = FULL || i < mine ? c : kNone;
+    }
+    if (a.softmax) {  // (z of a NaN is 0)
+#pragma unroll
+      for (int i = 0; i < PER; ++i) near_group = near_group || ((FULL || i < mine) && !(l[i] == l[i]));
     }
   } else {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       near_group = near_group || ((FULL || i < mine) && !(l[i] == l[i]));
-      key[i] = FULL || i < mine ? sort_key(__fadd_rn(l[i], 0.0f)) : 0u;  // (-0 as +0)
+      key[i] = FULL || i < mine ? l[i] : kNone;
     }
   }
-  uint32_t sorted[PER];
+  float sorted[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) sorted[i] = key[i];
   sort_desc<PER>(sorted);
+  bool keep = true;  // the lane's group stays
   if (a.G > 1) {
     // the two largest choices of the lane, then of its group
-    float t1 = sorted[0] != 0u ? key_value(sorted[0]) : kNone, t2 = PER > 1 && sorted[PER > 1 ? 1 : 0] != 0u ? key_value(sorted[PER > 1 ? 1 : 0]) : kNone;
+    float t1 = sorted[0], t2 = sorted[1];
     for (int d = a.lanes_per_group >> 1; d >= 1; d >>= 1) {
       const float o1 = __shfl_xor_sync(0xffffffffu, t1, d), o2 = __shfl_xor_sync(0xffffffffu, t2, d);
       t2 = fmaxf(fminf(t1, o1), fmaxf(t2, o2));
       t1 = fmaxf(t1, o1);
     }
     float group_slack = slack;
+    const float least = a.group_top == 2 ? t2 : t1;  // what an expert has to reach to count for its group
     if (a.group_top == 2) {
       if (a.bias == nullptr) {  // the order of scores is that of logits
         if (a.softmax) {
@@ -321,39 +405,50 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
       t1 += t2;
       group_slack *= 2.0f;
     }
-    // rounds over the groups: the lanes of the largest value are kept and drop out
+    // rounds over the groups: the lanes of the largest value drop out
     const int g = lane >> a.lanes_log2;
-    const uint32_t value = g < a.G ? order_key(topk_value(t1)) : 0u;
-    uint32_t left = value, last = 0u;
+    near_group = near_group || !(t1 == t1);
+    const float value = g < a.G ? t1 : kNone;
+    float left = value, last = kNone;
     for (int r = 0; r < a.top_groups; ++r) {
-      last = __reduce_max_sync(0xffffffffu, left);
-      left = left == last ? 0u : left;
+      last = reduce_max(left);
+      left = left == last ? kNone : left;
     }
-    const uint32_t next = __reduce_max_sync(0xffffffffu, left);
-    bool keep = value != 0u && left == 0u;
-    if (a.bias != nullptr || a.group_top == 2) {  // the border between the groups that stay and the others
-      near_group = near_group || next == 0u || near_choices(key_value(last), key_value(next), group_slack);
-    }
-    if (__popc(__ballot_sync(0xffffffffu, keep)) != a.top_groups << a.lanes_log2) {  // equal values: the lower groups
-      near_group = near_group || a.bias != nullptr || a.group_top == 2;               // (fp32 forms: decided again)
+    const float next = reduce_max(left);  // (every lane takes part, so not behind a condition of its own)
+    keep = g < a.G && value >= last;
+    if (last == kNone) {
+      near_group = true;
+    } else if (__popc(__ballot_sync(0xffffffffu, keep)) != a.top_groups << a.lanes_log2) {  // equal values: the lower groups
+      near_group = near_group || a.bias != nullptr || a.group_top == 2;                      // (fp32 forms: decided again)
       int before = 0;
 #pragma unroll 1
       for (int o = 0; o < a.G; ++o) {
-        const uint32_t v = __shfl_sync(0xffffffffu, value, o << a.lanes_log2);
-        before += v > value - (o < g ? 1u : 0u);  // (no key is zero)
+        const float v = __shfl_sync(0xffffffffu, value, o << a.lanes_log2);
+        before += v > value || (v == value && o < g);
       }
       keep = g < a.G && before < a.top_groups;
-    }
-    if (!keep) {
+    } else if ((a.bias != nullptr || a.group_top == 2) && near_choices(last, next, group_slack)) {
+      // Groups clearly above the best one that goes stay, groups clearly below the least one that stays go; between the others ...
+      const bool sure = keep && !near_choices(value, next, group_slack);
+      const bool question = g < a.G && !sure && (keep || near_choices(last, value, group_slack));
+      uint32_t mask = 0u;
 #pragma unroll
-      for (int i = 0; i < PER; ++i) key[i] = sorted[i] = 0u;
+      for (int i = 0; i < PER; ++i) {
+        const bool in = question && (FULL || i < mine) && (key[i] >= least || near_choices(least, key[i], 2.0f * slack));
+        mask |= in ? 1u << i : 0u;
+      }
+      bool decided;
+      keep = groups_exact<PER>(a, row, lane, first, mine, top, sure, question, mask, decided);
+      near_group = near_group || !decided;
     }
+    if (!keep) sorted[0] = kNone;  // (the others are not reached before -inf is the best there is)
   }
   // Rounds: lane r ends with the r-th largest key and the lanes that had it at their head.  Every lane that has the largest
   // key drops it, which is one lane unless keys are equal.
-  uint32_t my_key = 0u, my_lanes = 0u;
+  float my_key = kNone;
+  uint32_t my_lanes = 0u;
   for (int r = 0; r < a.K; ++r) {
-    const uint32_t best = __reduce_max_sync(0xffffffffu, sorted[0]);
+    const float best = reduce_max(sorted[0]);
     const bool mine_is_best = sorted[0] == best;
     const uint32_t lanes = __ballot_sync(0xffffffffu, mine_is_best);
     if (lane == r) {
@@ -362,25 +457,24 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
     }
 #pragma unroll
     for (int i = 0; i + 1 < PER; ++i) sorted[i] = mine_is_best ? sorted[i + 1] : sorted[i];
-    sorted[PER - 1] = mine_is_best ? 0u : sorted[PER - 1];
+    sorted[PER - 1] = mine_is_best ? kNone : sorted[PER - 1];
   }
   if (a.bias != nullptr) {
-    uint32_t after = __shfl_down_sync(0xffffffffu, my_key, 1);
-    const uint32_t next = __reduce_max_sync(0xffffffffu, sorted[0]);
+    float after = __shfl_down_sync(0xffffffffu, my_key, 1);
+    const float next = reduce_max(sorted[0]);
     if (lane == a.K - 1) after = next;
-    if (lane < a.K && after != 0u) near = near || near_choices(key_value(my_key), key_value(after), slack);
+    if (lane < a.K) near = near || near_choices(my_key, after, slack);
   }
-  // (with a bias, equal fp32 forms say nothing about the choices)
   const bool shared = lane < a.K && (my_lanes & (my_lanes - 1u)) != 0u;
-  near_group = __any_sync(0xffffffffu, near_group);
-  near = near_group || __any_sync(0xffffffffu, near || (a.bias != nullptr && shared));
-  if (!near && __any_sync(0xffffffffu, shared)) {
+  if (a.bias != nullptr) {
+    near = near || shared;  // equal fp32 forms say nothing about the choices
+  } else if (__any_sync(0xffffffffu, shared)) {
     // equal logits in several lanes (logits that were bf16 have them often): again, the lowest lane alone drops its key
 #pragma unroll
-    for (int i = 0; i < PER; ++i) sorted[i] = key[i];
+    for (int i = 0; i < PER; ++i) sorted[i] = keep ? key[i] : kNone;
     sort_desc<PER>(sorted);
     for (int r = 0; r < a.K; ++r) {
-      const uint32_t best = __reduce_max_sync(0xffffffffu, sorted[0]);
+      const float best = reduce_max(sorted[0]);
       const uint32_t lanes = __ballot_sync(0xffffffffu, sorted[0] == best), lowest = lanes & (0u - lanes);
       if (lane == r) {
         my_key = best;
@@ -389,34 +483,37 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
       if ((lowest >> lane) & 1u) {
 #pragma unroll
         for (int i = 0; i + 1 < PER; ++i) sorted[i] = sorted[i + 1];
-        sorted[PER - 1] = 0u;
+        sorted[PER - 1] = kNone;
       }
     }
   }
+  // (keys of -inf do not tell experts from places without one)
+  near_group = __any_sync(0xffffffffu, near_group || (lane < a.K && (my_key == kNone || my_lanes == 0u)));
+  near = near_group || __any_sync(0xffffffffu, near);
   int id;
   if (near) {
     // experts in question: choices that are not clearly below the K-th
-    const float least = key_value(__shfl_sync(0xffffffffu, my_key, a.K - 1));
+    const float least = __shfl_sync(0xffffffffu, my_key, a.K - 1);
     uint32_t mask = 0u;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const bool in = near_group ? FULL || i < mine : key[i] != 0u && (near_choices(least, key_value(key[i]), 2.0f * slack) || key_value(key[i]) >= least);
+      const bool in = (FULL || i < mine) && (near_group || (keep && (near_choices(least, key[i], 2.0f * slack) || key[i] >= least)));
       mask |= in ? 1u << i : 0u;
     }
     id = select_exact<PER>(a, row, lane, first, mine, top, mask, near_group && a.G > 1);
   } else {
     const int my_lane = (__ffs((int)my_lanes) - 1) & 31;
     int at = 0;
-    const uint32_t before = __shfl_up_sync(0xffffffffu, my_key, 1);
+    const float before = __shfl_up_sync(0xffffffffu, my_key, 1);
     if (!__any_sync(0xffffffffu, lane > 0 && lane < a.K && before == my_key)) {
 #pragma unroll
       for (int i = 1; i < PER; ++i) at = __shfl_sync(0xffffffffu, key[i], my_lane) == my_key ? i : at;
     } else {  // equal keys of one lane are taken in the order of their indices
-      const uint32_t same = __match_any_sync(0xffffffffu, my_key) & __match_any_sync(0xffffffffu, my_lane);
+      const uint32_t same = __match_any_sync(0xffffffffu, __float_as_uint(__fadd_rn(my_key, 0.0f))) & __match_any_sync(0xffffffffu, my_lane);
       int skip = __popc(same & ((1u << lane) - 1u));
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const uint32_t k = __shfl_sync(0xffffffffu, key[i], my_lane);
+        const float k = __shfl_sync(0xffffffffu, key[i], my_lane);
         if (k == my_key) {
           if (skip == 0) at = i;
           --skip;

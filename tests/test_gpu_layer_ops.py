@@ -154,6 +154,28 @@ def test_route_groups_of_equal_fp32_value(b):
 
 
 @pytest.mark.parametrize("score", [0, 1])
+@pytest.mark.parametrize("e,groups,top_groups,k,alike", [(64, 8, 3, 8, 2), (64, 8, 1, 5, 8), (512, 16, 9, 32, 2), (96, 3, 2, 6, 4), (40, 20, 7, 3, 2), (512, 32, 30, 8, 3)])
+def test_route_groups_whose_border_fp32_cannot_tell(b, score, e, groups, top_groups, k, alike):
+    """Groups whose best experts differ by a few units in the last place; of some tokens all groups, of others those around the border.
+    `alike` experts of a group are that near to each other's counterparts (and, in every second token, to each other)."""
+    rng = np.random.default_rng(9)
+    t, size = 120, e // groups
+    logits = rng.uniform(-3, 0, size=(t, groups, size)).astype(np.float32)
+    for i in range(t):
+        best = np.full(alike, 1.5) if i % 2 else 1.0 + 0.5 * np.arange(alike)
+        for g in range(groups):
+            at = rng.choice(size, min(alike, size), replace=False)
+            logits[i, g, at] = best[:len(at)].astype(np.float32) + (rng.integers(-2, 3, size=len(at)) * 2.0 ** -23).astype(np.float32)
+        if i % 3:
+            far = rng.choice(groups, groups // 2, replace=False)
+            logits[i, far] += rng.choice([-0.5, 0.5], size=(len(far), 1)).astype(np.float32)
+    logits = logits.reshape(t, e)
+    for bias in (None, np.zeros(e, np.float32), np.full(e, 0.25, np.float32)):
+        for group_top in (1, 2):
+            check_route(b, logits, bias, top_k=k, score=score, n_groups=groups, top_groups=top_groups, group_top=group_top)
+
+
+@pytest.mark.parametrize("score", [0, 1])
 def test_route_non_finite(b, score):
     rng = np.random.default_rng(6)
     e = 32
