@@ -54,11 +54,6 @@ struct ScoredArgs {
   const float* conf;
 };
 
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-  for (int d = 16; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
-  return v;
-}
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
@@ -309,6 +304,14 @@ __device__ __forceinline__ float fast_reciprocal(float x) {
 }
 __device__ __forceinline__ float fast_sigmoid(float l) { return fast_reciprocal(1.0f + fast_exp(-l)); }
 
+// Where the bias of a lane's expert i lies in shared memory, so that a warp reads up to 16 bytes a lane at once.  (In registers they left too few
+// for the rest.)
+template <int PER>
+__device__ __forceinline__ int bias_at(int lane, int i) {
+  constexpr int kRun = PER < 4 ? PER : 4;
+  return (i / kRun * 32 + lane) * kRun + i % kRun;
+}
+
 // A token's logits, as its lanes hold them.  PER: experts a lane has room for.  FULL: every lane has that many.
 template <int PER, bool FULL>
 __device__ __forceinline__ void load_logits(const ScoredArgs& a, int t, int first, int mine, float (&l)[PER]) {
@@ -331,7 +334,7 @@ __device__ __forceinline__ void load_logits(const ScoredArgs& a, int t, int firs
 }
 
 template <int PER, bool FULL>
-__device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane, const float (&l)[PER], const float (&bias)[PER], int first,
+__device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane, const float (&l)[PER], const float* s_bias, int first,
                                             int mine_, int32_t* s_ids, int32_t* s_counts, unsigned long long* s_scores) {
   const int mine = FULL ? PER : mine_;
   const float* const row = a.logits + (int64_t)t * a.stride;
@@ -345,19 +348,25 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
 #pragma unroll
     for (int i = 0; i < PER; ++i)
       if (FULL || i < mine) top = fmaxf(top, l[i]);
-    top = warp_max(top);
-    sum = 0.0f;
+    top = reduce_max(top);
+    // (renormalised weights are quotients of the chosen exponentials, and the largest of those is 1: 1e-20 beside it is nothing)
+    if (a.bias != nullptr || !a.renormalise || a.G > 1) {
+      sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const float x = fmaxf(l[i], kNone);
-      z[i] = FULL || i < mine ? (x == top ? 1.0f : fast_exp(x - top)) : 0.0f;
-      sum += z[i];
+      for (int i = 0; i < PER; ++i) {
+        const float x = fmaxf(l[i], kNone);
+        z[i] = FULL || i < mine ? (x == top ? 1.0f : fast_exp(x - top)) : 0.0f;
+        sum += z[i];
+      }
+      sum = warp_sum(sum);
     }
-    sum = warp_sum(sum);
   }
   const float inverse = fast_reciprocal(sum);
   if (a.bias != nullptr) {
     slack = a.softmax ? 9.2e-6f * inverse : 5.8e-7f;
+    float bias[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) bias[i] = s_bias[bias_at<PER>(lane, i)];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const float c = (a.softmax ? z[i] * inverse : fast_sigmoid(l[i])) + bias[i];
@@ -543,7 +552,7 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
 
 // The tokens begin + warp, begin + warp + kScoredWarps, ... of a CTA; the next one's logits are on their way while one is routed.
 template <int PER, bool FULL>
-__device__ __forceinline__ void route_tokens(const ScoredArgs& a, int begin, int end, int warp, int lane, const float (&bias)[PER], int first,
+__device__ __forceinline__ void route_tokens(const ScoredArgs& a, int begin, int end, int warp, int lane, const float* s_bias, int first,
                                              int mine, int32_t* s_ids, int32_t* s_counts, unsigned long long* s_scores) {
   float l[PER];
   int t = begin + warp;
@@ -553,18 +562,22 @@ __device__ __forceinline__ void route_tokens(const ScoredArgs& a, int begin, int
 #pragma unroll
     for (int i = 0; i < PER; ++i) now[i] = l[i];
     if (t + kScoredWarps < end) load_logits<PER, FULL>(a, t + kScoredWarps, first, mine, l);
-    route_token<PER, FULL>(a, t, lane, now, bias, first, mine, s_ids != nullptr ? s_ids + (t - begin) * a.K : nullptr, s_counts, s_scores);
+    route_token<PER, FULL>(a, t, lane, now, s_bias, first, mine, s_ids != nullptr ? s_ids + (t - begin) * a.K : nullptr, s_counts, s_scores);
   }
 }
 
-// The experts of a lane, and their biases.
-template <int PER>
-__device__ __forceinline__ void lane_experts(const ScoredArgs& a, int lane, int& first, int& mine, float (&bias)[PER]) {
+// The experts of a lane.
+__device__ __forceinline__ void lane_experts(const ScoredArgs& a, int lane, int& first, int& mine) {
   const int g = lane >> a.lanes_log2, sub = lane - (g << a.lanes_log2);
   first = g < a.G ? g * a.group_size + sub * a.per_lane : 0;
   mine = g < a.G ? max(0, min(a.per_lane, a.group_size - sub * a.per_lane)) : 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) bias[i] = a.bias != nullptr && i < mine ? a.bias[first + i] : 0.0f;
+}
+// The lanes' biases to shared memory.
+template <int PER>
+__device__ __forceinline__ void fetch_bias(const ScoredArgs& a, int warp, int lane, int first, int mine, float* s_bias) {
+  if (a.bias == nullptr) return;
+  for (int i = warp; i < PER; i += kScoredWarps) s_bias[bias_at<PER>(lane, i)] = i < mine ? a.bias[first + i] : 0.0f;
+  __syncthreads();
 }
 
 // Dynamic shared memory: [E] scores (where wanted), [E] counts (where wanted).
@@ -586,12 +599,13 @@ route_scored_kernel(const __grid_constant__ ScoredArgs a) {
   }
   griddep_wait();
   int first, mine;
-  float bias[PER];
-  lane_experts<PER>(a, lane, first, mine, bias);
+  __shared__ __align__(16) float s_bias[32 * PER];
+  lane_experts(a, lane, first, mine);
+  fetch_bias<PER>(a, warp, lane, first, mine, s_bias);
   const int seg = (int)blockIdx.x / a.parts, part = (int)blockIdx.x - seg * a.parts;
   const int begin = seg * a.seg_tokens + part * a.part_tokens;
   const int end = min(min(begin + a.part_tokens, (seg + 1) * a.seg_tokens), a.T);
-  route_tokens<PER, FULL>(a, begin, end, warp, lane, bias, first, mine, nullptr, s_counts, s_scores);
+  route_tokens<PER, FULL>(a, begin, end, warp, lane, s_bias, first, mine, nullptr, s_counts, s_scores);
   if (!counting) return;
   __syncthreads();
   for (int e = threadIdx.x; e < a.E; e += kScoredThreads) {
@@ -724,10 +738,11 @@ route_cluster_kernel(const __grid_constant__ ScoredArgs a, int32_t* __restrict__
   for (int i = threadIdx.x; i < kScoredWarps * a.E; i += kScoredThreads) s_rows[i] = 0;
   griddep_wait();
   int first, mine;
-  float bias[PER];
-  lane_experts<PER>(a, lane, first, mine, bias);
+  __shared__ __align__(16) float s_bias[32 * PER];
+  lane_experts(a, lane, first, mine);
+  fetch_bias<PER>(a, warp, lane, first, mine, s_bias);
   const int begin = min(rank * a.part_tokens, a.T), end = min(begin + a.part_tokens, a.T);
-  route_tokens<PER, FULL>(a, begin, end, warp, lane, bias, first, mine, s_ids, nullptr, nullptr);
+  route_tokens<PER, FULL>(a, begin, end, warp, lane, s_bias, first, mine, s_ids, nullptr, nullptr);
   __syncthreads();
   place_rows(s_ids, (end - begin) * a.K, (int64_t)begin * a.K, a.E, s_rows, perm, [&](int e, int total) {
     int all = total, before = 0;
