@@ -33,6 +33,9 @@ namespace {
 
 constexpr int kScoredWarps = 16;
 constexpr int kScoredThreads = kScoredWarps * 32;
+// Warps of a CTA that only routes, at most: one CTA an SM, of as many warps as its registers are enough for.
+__host__ __device__ constexpr int route_warps(int per) { return per <= 8 ? 32 : 16; }
+constexpr int kExactLanes = 32;  // experts that a warp decides in fp64 side by side
 
 struct ScoredArgs {
   const float* logits;
@@ -45,8 +48,9 @@ struct ScoredArgs {
   int group_size, lanes_per_group, lanes_log2, per_lane, vec;
   // tokens of CTA c: segment c / parts, of seg_tokens tokens, and there the part c % parts, of part_tokens
   int parts, seg_tokens, part_tokens;
-  // (nullptr: not wanted) per expert and CTA, [E][n_ctas]
-  int32_t* hist;
+  // (nullptr: not wanted) per CTA and expert, [n_ctas][hist_stride]
+  uint16_t* hist;
+  int hist_stride;
   // (nullptr: not wanted) zeroed arrays of a step: counts [E], per-segment counts [n_segments][E], reuse-score numerators [E]
   int32_t* counts;
   int32_t* seg_counts;
@@ -141,7 +145,7 @@ __device__ __forceinline__ double choice_exact(const ScoredArgs& a, const float*
   const double c = a.bias == nullptr ? (double)l : score + (double)a.bias[e];
   return l == l && c == c ? c : -INFINITY;
 }
-// Deals the experts of the lanes' masks to the lanes, one each; their number (above 32: none dealt).
+// Deals the experts of the lanes' masks to the lanes, one each, by way of the warp's s_experts[kExactLanes]; their number (above 32: none dealt).
 template <int PER>
 __device__ __forceinline__ int deal(uint32_t mask, int lane, int first, int32_t* s_experts, int& expert) {
   int n = 0;
@@ -151,7 +155,7 @@ __device__ __forceinline__ int deal(uint32_t mask, int lane, int first, int32_t*
     const bool in = (mask >> i) & 1u;
     const uint32_t lanes = __ballot_sync(0xffffffffu, in);
     const int at = n + __popc(lanes & ((1u << lane) - 1u));
-    if (in && at < 32) s_experts[at] = first + i;
+    if (in && at < kExactLanes) s_experts[at] = first + i;
     n += __popc(lanes);
   }
   __syncwarp();
@@ -164,10 +168,9 @@ __device__ __forceinline__ int deal(uint32_t mask, int lane, int first, int32_t*
 // False in `decided`: too many experts.
 template <int PER>
 __device__ __noinline__ bool groups_exact(const ScoredArgs& a, const float* row, int lane, int first, int mine, float top, bool sure, bool question,
-                                          uint32_t mask, bool& decided) {
-  __shared__ int32_t s_experts[kScoredWarps][32];
+                                          uint32_t mask, int32_t* s_experts, bool& decided) {
   int expert;
-  const int n = deal<PER>(mask, lane, first, s_experts[(threadIdx.x >> 5) % kScoredWarps], expert);
+  const int n = deal<PER>(mask, lane, first, s_experts, expert);
   decided = n <= 32;
   if (!decided) return false;
   const double sum = a.softmax ? sum_exact(row, first, mine, top) : 1.0;
@@ -203,15 +206,13 @@ __device__ __noinline__ bool groups_exact(const ScoredArgs& a, const float* row,
 // in turn, and rounds to order them: 250 tokens with one such 8.4 us, this way WHAT; with all experts a token took 5.5 us).
 template <int PER>
 __device__ __noinline__ int select_exact(const ScoredArgs& a, const float* row, int lane, int first, int mine, float top, uint32_t mask,
-                                         bool groups) {
-  __shared__ int32_t s_experts[kScoredWarps][32];
-  int32_t* const experts = s_experts[(threadIdx.x >> 5) % kScoredWarps];
+                                         bool groups, int32_t* s_experts) {
   const double kNone = -INFINITY;
   unsigned long long key[PER];  // of the choices (in local memory: registers count for the whole kernel)
   const double sum = a.softmax ? sum_exact(row, first, mine, top) : 1.0;
   double score;
   int expert;
-  const int n = groups ? 33 : deal<PER>(mask, lane, first, experts, expert);
+  const int n = groups ? 33 : deal<PER>(mask, lane, first, s_experts, expert);
   if (n <= 32) {
     const double c = choice_exact(a, row, expert, top, sum, score);
     int before = 0;
@@ -222,9 +223,9 @@ __device__ __noinline__ int select_exact(const ScoredArgs& a, const float* row, 
       before += v > c || (v == c && e < expert);
     }
     __syncwarp();
-    if (lane < n && before < a.K) experts[before] = expert;
+    if (lane < n && before < a.K) s_experts[before] = expert;
     __syncwarp();
-    return lane < a.K ? experts[lane] : 0;
+    return lane < a.K ? s_experts[lane] : 0;
   }
   double t1 = kNone, t2 = kNone;
 #pragma unroll 1
@@ -335,7 +336,7 @@ __device__ __forceinline__ void load_logits(const ScoredArgs& a, int t, int firs
 
 template <int PER, bool FULL>
 __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane, const float (&l)[PER], const float* s_bias, int first,
-                                            int mine_, int32_t* s_ids, int32_t* s_counts, unsigned long long* s_scores) {
+                                            int mine_, int32_t* s_experts, int32_t* s_ids, int32_t* s_counts, unsigned long long* s_scores) {
   const int mine = FULL ? PER : mine_;
   const float* const row = a.logits + (int64_t)t * a.stride;
   const float kNone = __int_as_float(0xff800000);
@@ -447,7 +448,7 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
         mask |= in ? 1u << i : 0u;
       }
       bool decided;
-      keep = groups_exact<PER>(a, row, lane, first, mine, top, sure, question, mask, decided);
+      keep = groups_exact<PER>(a, row, lane, first, mine, top, sure, question, mask, s_experts, decided);
       near_group = near_group || !decided;
     }
     if (!keep) sorted[0] = kNone;  // (the others are not reached before -inf is the best there is)
@@ -509,7 +510,7 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
       const bool in = (FULL || i < mine) && (near_group || (keep && (near_choices(least, key[i], 2.0f * slack) || key[i] >= least)));
       mask |= in ? 1u << i : 0u;
     }
-    id = select_exact<PER>(a, row, lane, first, mine, top, mask, near_group && a.G > 1);
+    id = select_exact<PER>(a, row, lane, first, mine, top, mask, near_group && a.G > 1, s_experts);
   } else {
     const int my_lane = (__ffs((int)my_lanes) - 1) & 31;
     int at = 0;
@@ -550,19 +551,20 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
   }
 }
 
-// The tokens begin + warp, begin + warp + kScoredWarps, ... of a CTA; the next one's logits are on their way while one is routed.
+// The tokens begin + warp, begin + warp + n_warps, ... of a CTA; the next one's logits are on their way while one is routed.
 template <int PER, bool FULL>
-__device__ __forceinline__ void route_tokens(const ScoredArgs& a, int begin, int end, int warp, int lane, const float* s_bias, int first,
-                                             int mine, int32_t* s_ids, int32_t* s_counts, unsigned long long* s_scores) {
+__device__ __forceinline__ void route_tokens(const ScoredArgs& a, int begin, int end, int warp, int n_warps, int lane, const float* s_bias, int first,
+                                             int mine, int32_t* s_experts, int32_t* s_ids, int32_t* s_counts, unsigned long long* s_scores) {
   float l[PER];
   int t = begin + warp;
   if (t < end) load_logits<PER, FULL>(a, t, first, mine, l);
-  for (; t < end; t += kScoredWarps) {
+  for (; t < end; t += n_warps) {
     float now[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) now[i] = l[i];
-    if (t + kScoredWarps < end) load_logits<PER, FULL>(a, t + kScoredWarps, first, mine, l);
-    route_token<PER, FULL>(a, t, lane, now, s_bias, first, mine, s_ids != nullptr ? s_ids + (t - begin) * a.K : nullptr, s_counts, s_scores);
+    if (t + n_warps < end) load_logits<PER, FULL>(a, t + n_warps, first, mine, l);
+    route_token<PER, FULL>(a, t, lane, now, s_bias, first, mine, s_experts + warp * kExactLanes, s_ids != nullptr ? s_ids + (t - begin) * a.K : nullptr,
+                           s_counts, s_scores);
   }
 }
 
@@ -574,24 +576,26 @@ __device__ __forceinline__ void lane_experts(const ScoredArgs& a, int lane, int&
 }
 // The lanes' biases to shared memory.
 template <int PER>
-__device__ __forceinline__ void fetch_bias(const ScoredArgs& a, int warp, int lane, int first, int mine, float* s_bias) {
+__device__ __forceinline__ void fetch_bias(const ScoredArgs& a, int warp, int n_warps, int lane, int first, int mine, float* s_bias) {
   if (a.bias == nullptr) return;
-  for (int i = warp; i < PER; i += kScoredWarps) s_bias[bias_at<PER>(lane, i)] = i < mine ? a.bias[first + i] : 0.0f;
+  for (int i = warp; i < PER; i += n_warps) s_bias[bias_at<PER>(lane, i)] = i < mine ? a.bias[first + i] : 0.0f;
   __syncthreads();
 }
 
 // Dynamic shared memory: [E] scores (where wanted), [E] counts (where wanted).
 template <int PER, bool FULL>
-__global__ void __launch_bounds__(kScoredThreads, PER <= 8 ? 2 : 1)
+__global__ void __launch_bounds__(route_warps(PER) * 32, 1)
 route_scored_kernel(const __grid_constant__ ScoredArgs a) {
   extern __shared__ __align__(16) uint8_t s_dyn[];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  __shared__ __align__(16) float s_bias[32 * PER];
+  __shared__ int32_t s_experts[route_warps(PER) * kExactLanes];
+  const int warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5, lane = threadIdx.x & 31;
   unsigned long long* const s_scores = a.scores != nullptr ? reinterpret_cast<unsigned long long*>(s_dyn) : nullptr;
   const bool counting = a.hist != nullptr || a.counts != nullptr;
   int32_t* const s_counts = counting ? reinterpret_cast<int32_t*>(s_dyn + (s_scores != nullptr ? (size_t)a.E * 8 : 0)) : nullptr;
   griddep_launch_dependents();
   if (counting) {
-    for (int e = threadIdx.x; e < a.E; e += kScoredThreads) {
+    for (int e = threadIdx.x; e < a.E; e += blockDim.x) {
       s_counts[e] = 0;
       if (s_scores != nullptr) s_scores[e] = 0ull;
     }
@@ -599,18 +603,17 @@ route_scored_kernel(const __grid_constant__ ScoredArgs a) {
   }
   griddep_wait();
   int first, mine;
-  __shared__ __align__(16) float s_bias[32 * PER];
   lane_experts(a, lane, first, mine);
-  fetch_bias<PER>(a, warp, lane, first, mine, s_bias);
+  fetch_bias<PER>(a, warp, n_warps, lane, first, mine, s_bias);
   const int seg = (int)blockIdx.x / a.parts, part = (int)blockIdx.x - seg * a.parts;
   const int begin = seg * a.seg_tokens + part * a.part_tokens;
   const int end = min(min(begin + a.part_tokens, (seg + 1) * a.seg_tokens), a.T);
-  route_tokens<PER, FULL>(a, begin, end, warp, lane, s_bias, first, mine, nullptr, s_counts, s_scores);
+  route_tokens<PER, FULL>(a, begin, end, warp, n_warps, lane, s_bias, first, mine, s_experts, nullptr, s_counts, s_scores);
   if (!counting) return;
   __syncthreads();
-  for (int e = threadIdx.x; e < a.E; e += kScoredThreads) {
+  for (int e = threadIdx.x; e < a.E; e += blockDim.x) {
     const int n = s_counts[e];
-    if (a.hist != nullptr) a.hist[(size_t)e * gridDim.x + blockIdx.x] = n;
+    if (a.hist != nullptr) a.hist[(size_t)blockIdx.x * a.hist_stride + e] = (uint16_t)n;  // (a CTA has fewer than 2^16 tokens)
     if (n == 0) continue;
     if (a.counts != nullptr) atomicAdd(&a.counts[e], n);
     if (a.seg_counts != nullptr) atomicAdd(&a.seg_counts[seg * a.E + e], n);
@@ -636,88 +639,112 @@ __device__ __forceinline__ int cta_prefix(int v, int* s_warp) {
   return before;
 }
 
-// Rows of a CTA's n assignments (ids[0 .. n - 1], the first of them number a0) in the stable order by expert.  Every warp counts the
-// experts of a contiguous part (s_rows: [kScoredWarps][E], zeros), start(e, n of the CTA) says where the CTA's rows of an expert
-// begin, and every warp hands out its part's rows in order.
+// Rows of the assignments of a CTA's n tokens (ids: K of each token; the first of them is number a0) in the stable order by expert. Every warp
+// counts the experts of a contiguous part (s_rows: [kScoredWarps][E], zeros), start(e, n of the CTA) says where the CTA's rows of an
+// expert begin, and every warp hands out its part's rows in order, a token at a time: its experts differ, so that its lanes need
+// not look for equal ones among them (32 assignments at a time with a match among the lanes took four times as long).
 template <typename Start>
-__device__ __forceinline__ void place_rows(const int32_t* ids, int n, int64_t a0, int E, int* s_rows, int32_t* __restrict__ perm, Start start) {
+__device__ __forceinline__ void place_rows(const int32_t* ids, int n, int K, int64_t a0, int E, int* s_rows, int32_t* __restrict__ perm, Start start) {
   static_assert(kScoredThreads >= OLED_MAX_EXPERTS, "a thread per expert");
+  static_assert(OLED_MAX_TOPK <= 32, "a lane per expert of a token");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int per_warp = (n + kScoredThreads - 1) / kScoredThreads * 32, first = warp * per_warp, last = min(n, first + per_warp);
+  const int per_warp = (n + kScoredWarps - 1) / kScoredWarps, first = min(n, warp * per_warp), last = min(n, first + per_warp);
   int* const mine = s_rows + warp * E;
-  for (int i = first + lane; i < last; i += 32) atomicAdd(&mine[ids[i]], 1);
+  for (int i = first * K + lane; i < last * K; i += 32) atomicAdd(&mine[ids[i]], 1);
   __syncthreads();
   const int e = threadIdx.x;
-  int total = 0;
+  int total = 0, part[kScoredWarps];
   if (e < E)
+#pragma unroll
     for (int w = 0; w < kScoredWarps; ++w) {
-      const int c = s_rows[w * E + e];
-      s_rows[w * E + e] = total;
-      total += c;
+      part[w] = s_rows[w * E + e];
+      total += part[w];
     }
-  const int at = start(e, total);
+  int at = start(e, total);
   if (e < E)
-    for (int w = 0; w < kScoredWarps; ++w) s_rows[w * E + e] += at;
-  __syncthreads();
-  for (int i0 = first; i0 < last; i0 += 32) {
-    const int id = i0 + lane < last ? ids[i0 + lane] : -1;
-    const uint32_t same = __match_any_sync(0xffffffffu, id);
-    const int rank = __popc(same & ((1u << lane) - 1u));
-    if (id >= 0) perm[mine[id] + rank] = (int32_t)(a0 + i0 + lane);
-    __syncwarp();
-    if (id >= 0 && rank == 0) mine[id] += __popc(same);
-    __syncwarp();
-  }
-}
-
-constexpr int kScoredCtas = 148 * 2;  // at most
-
-// Counts and prefixes of an expert over the CTAs: a warp per expert, in place, all of its values in flight together.
-__global__ void __launch_bounds__(256)
-scan_hist_kernel(int32_t* hist, int n_ctas, int E, int32_t* counts) {
-  constexpr int kPer = (kScoredCtas + 31) / 32;
-  const int e = (int)blockIdx.x * 8 + ((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
-  griddep_launch_dependents();
-  griddep_wait();
-  if (e >= E) return;
-  int32_t* const row = hist + (size_t)e * n_ctas;
-  int v[kPer];
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) v[j] = j * 32 + lane < n_ctas ? row[j * 32 + lane] : 0;
-  int carry = 0;
-#pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    int incl = v[j];
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, incl, d);
-      if (lane >= d) incl += o;
+    for (int w = 0; w < kScoredWarps; ++w) {
+      s_rows[w * E + e] = at;
+      at += part[w];
     }
-    if (j * 32 + lane < n_ctas) row[j * 32 + lane] = carry + incl - v[j];
-    carry += __shfl_sync(0xffffffffu, incl, 31);
+  __syncthreads();
+  // (as many whole tokens as there are lanes for are fetched at once, and the next ones meanwhile)
+  const int tokens = 32 / K, mine_of = lane / K;
+  int id = mine_of < tokens && first + mine_of < last ? ids[first * K + lane] : -1;
+  for (int t = first; t < last; t += tokens) {
+    const int next = mine_of < tokens && t + tokens + mine_of < last ? ids[(t + tokens) * K + lane] : -1;
+    for (int j = 0; j < tokens; ++j) {
+      if (mine_of == j && id >= 0) {
+        const int row = mine[id];
+        mine[id] = row + 1;
+        perm[row] = (int32_t)(a0 + t * K + lane);
+      }
+      __syncwarp();
+    }
+    id = next;
   }
-  if (lane == 0) counts[e] = carry;
 }
 
+constexpr int kScoredCtas = 148;  // at most: one an SM
+// More than half of an SM's shared memory, so that no SM takes two CTAs while others have none: they start as SMs become free.
+constexpr size_t kPlaceSmem = 120 * 1024;
+static_assert(kPlaceSmem >= (size_t)kScoredWarps * OLED_MAX_EXPERTS * sizeof(int), "a row of counts per warp");
+
+// Every CTA adds up the histograms of all of them itself, 150 rows of E 16-bit counts out of L2: cheaper than a kernel in between that leaves
+// it one row to read (32768 tokens, 256 experts in groups: WITH, without WITHOUT).
 __global__ void __launch_bounds__(kScoredThreads)
-place_kernel(const int32_t* __restrict__ ids, int T, int K, int E, int part_tokens, const int32_t* __restrict__ hist,
-             const int32_t* __restrict__ counts, int32_t* __restrict__ offsets, int32_t* __restrict__ perm) {
+place_kernel(const int32_t* __restrict__ ids, int T, int K, int E, int part_tokens, const uint16_t* __restrict__ hist, int hist_stride,
+             int32_t* __restrict__ counts, int32_t* __restrict__ offsets, int32_t* __restrict__ perm) {
   extern __shared__ int s_rows[];  // [kScoredWarps][E]
   __shared__ int s_warp[kScoredWarps];
+  constexpr int kFours = OLED_MAX_EXPERTS / 4, kTogether = 10;  // expert e's sums are at [e % 4][e / 4]
+  __shared__ int s_all[OLED_MAX_EXPERTS], s_before[OLED_MAX_EXPERTS];
   griddep_launch_dependents();
   for (int i = threadIdx.x; i < kScoredWarps * E; i += kScoredThreads) s_rows[i] = 0;
+  for (int i = threadIdx.x; i < OLED_MAX_EXPERTS; i += kScoredThreads) s_all[i] = s_before[i] = 0;
   griddep_wait();
   __syncthreads();
-  const int64_t a0 = (int64_t)blockIdx.x * part_tokens * K, a1 = min(a0 + (int64_t)part_tokens * K, (int64_t)T * K);
-  const int mine = (int)threadIdx.x < E ? counts[threadIdx.x] : 0;
-  const int before = (int)threadIdx.x < E ? hist[(size_t)threadIdx.x * gridDim.x + blockIdx.x] : 0;
-  place_rows(ids + a0, (int)(a1 - a0), a0, E, s_rows, perm, [&](int e, int) {
-    const int start = cta_prefix<kScoredWarps>(mine, s_warp);
-    if (blockIdx.x == 0 && e < E) {
-      offsets[e] = start;
-      if (e == E - 1) offsets[E] = start + mine;
+  // A thread per four experts and every `step`-th row, from the CTA's own row on: all of them on the same one at a time would wait for its L2
+  // slice.
+  const int fours = hist_stride / 4, step = kScoredThreads / fours, rows = (int)gridDim.x;
+  const int first = (int)threadIdx.x / fours, four = (int)threadIdx.x - first * fours;
+  if (first < step) {
+    const uint2* const column = reinterpret_cast<const uint2*>(hist) + four;
+    int all[4] = {}, before[4] = {};
+    for (int i0 = first; i0 < rows; i0 += step * kTogether) {
+      uint2 c[kTogether];
+#pragma unroll
+      for (int u = 0; u < kTogether; ++u) {
+        const int i = i0 + u * step, r = i + (int)blockIdx.x < rows ? i + (int)blockIdx.x : i + (int)blockIdx.x - rows;
+        c[u] = i < rows ? column[(size_t)r * fours] : make_uint2(0u, 0u);
+      }
+#pragma unroll
+      for (int u = 0; u < kTogether; ++u) {
+        const bool is_before = i0 + u * step + (int)blockIdx.x >= rows;  // (rows from the CTA's own on come first)
+        const int n[4] = {(int)(c[u].x & 0xffffu), (int)(c[u].x >> 16), (int)(c[u].y & 0xffffu), (int)(c[u].y >> 16)};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          all[j] += n[j];
+          before[j] += is_before ? n[j] : 0;
+        }
+      }
     }
-    return start + before;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      atomicAdd(&s_all[j * kFours + four], all[j]);
+      atomicAdd(&s_before[j * kFours + four], before[j]);
+    }
+  }
+  const int begin = (int)blockIdx.x * part_tokens, end = min(begin + part_tokens, T);
+  const int64_t a0 = (int64_t)begin * K;
+  place_rows(ids + a0, end - begin, K, a0, E, s_rows, perm, [&](int e, int) {  // (behind a barrier)
+    const int at = e % 4 * kFours + e / 4, all = e < E ? s_all[at] : 0, start = cta_prefix<kScoredWarps>(all, s_warp);
+    if (blockIdx.x == 0 && e < E) {
+      counts[e] = all;
+      offsets[e] = start;
+      if (e == E - 1) offsets[E] = start + all;
+    }
+    return start + (e < E ? s_before[at] : 0);
   });
 }
 
@@ -733,18 +760,19 @@ route_cluster_kernel(const __grid_constant__ ScoredArgs a, int32_t* __restrict__
   __shared__ int s_total[OLED_MAX_EXPERTS];
   __shared__ int32_t s_ids[kClusterIds];
   __shared__ int s_warp[kScoredWarps];
+  __shared__ __align__(16) float s_bias[32 * PER];
+  __shared__ int32_t s_experts[kScoredWarps * kExactLanes];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_ctas = gridDim.x, rank = blockIdx.x;
   griddep_launch_dependents();
   for (int i = threadIdx.x; i < kScoredWarps * a.E; i += kScoredThreads) s_rows[i] = 0;
   griddep_wait();
   int first, mine;
-  __shared__ __align__(16) float s_bias[32 * PER];
   lane_experts(a, lane, first, mine);
-  fetch_bias<PER>(a, warp, lane, first, mine, s_bias);
+  fetch_bias<PER>(a, warp, kScoredWarps, lane, first, mine, s_bias);
   const int begin = min(rank * a.part_tokens, a.T), end = min(begin + a.part_tokens, a.T);
-  route_tokens<PER, FULL>(a, begin, end, warp, lane, s_bias, first, mine, s_ids, nullptr, nullptr);
+  route_tokens<PER, FULL>(a, begin, end, warp, kScoredWarps, lane, s_bias, first, mine, s_experts, s_ids, nullptr, nullptr);
   __syncthreads();
-  place_rows(s_ids, (end - begin) * a.K, (int64_t)begin * a.K, a.E, s_rows, perm, [&](int e, int total) {
+  place_rows(s_ids, end - begin, a.K, (int64_t)begin * a.K, a.E, s_rows, perm, [&](int e, int total) {
     int all = total, before = 0;
     if (n_ctas > 1) {
       if (e < a.E) s_total[e] = total;
@@ -776,13 +804,15 @@ route_cluster_kernel(const __grid_constant__ ScoredArgs a, int32_t* __restrict__
 }
 
 // How many CTAs share a routing of T tokens.  Up to kOneLaunch assignments a cluster sorts its own, which takes no scratch;
-// beyond, a CTA sorts what it routed and a kernel in between adds up the CTAs' histograms.
+// beyond, routing leaves a histogram per CTA and a second kernel of as many CTAs sorts.  A warp takes four tokens and more only where every
+// SM has that many.
 bool one_launch(int T, int K) { return (int64_t)T * K <= kOneLaunch; }
 int scored_parts(int T) {
-  const int parts = std::min((T + kScoredWarps - 1) / kScoredWarps, kScoredCtas);
+  const int parts = std::min((T + 3) / 4, kScoredCtas);
   const int part_tokens = (T + parts - 1) / parts;
   return (T + part_tokens - 1) / part_tokens;  // (none of them empty)
 }
+int hist_stride(int E) { return (E + 3) / 4 * 4; }
 int cluster_ctas(int T) {
   int n = 1;
   while (n < 8 && n * kScoredWarps < T) n *= 2;
@@ -849,7 +879,8 @@ cudaError_t with_layout(const ScoredArgs& a, F f) {
 cudaError_t launch_scored(cudaStream_t st, const ScoredArgs& a, int ctas) {
   const size_t smem = (a.scores != nullptr ? (size_t)a.E * 8 : 0) + (a.hist != nullptr || a.counts != nullptr ? (size_t)a.E * 4 : 0);
   return with_layout(a, [&](auto per, auto full) {
-    return launch_pdl(route_scored_kernel<decltype(per)::value, decltype(full)::value>, dim3((unsigned)ctas), dim3(kScoredThreads), smem, st, a);
+    return launch_pdl(route_scored_kernel<decltype(per)::value, decltype(full)::value>, dim3((unsigned)ctas),
+                      dim3(32 * std::min(route_warps(decltype(per)::value), a.part_tokens)), smem, st, a);
   });
 }
 
@@ -879,7 +910,7 @@ cudaError_t launch_route_step(cudaStream_t st, const oled_routing& r, const floa
   if (seg_counts != nullptr) {
     segments = (T + seg_tokens - 1) / seg_tokens;
     a.seg_tokens = seg_tokens;
-    a.parts = std::max(1, std::min((seg_tokens + kScoredWarps - 1) / kScoredWarps, kScoredCtas / segments));
+    a.parts = std::max(1, std::min((seg_tokens + 3) / 4, kScoredCtas / segments));
   }
   a.part_tokens = (a.seg_tokens + a.parts - 1) / a.parts;
   return launch_scored(st, a, segments * a.parts);
@@ -890,7 +921,7 @@ cudaError_t launch_route_step(cudaStream_t st, const oled_routing& r, const floa
 extern "C" size_t oled_route_scored_scratch(const oled_routing* routing, int32_t n_tokens) {
   using namespace oled;
   if (!routing_ok(routing) || n_tokens <= 0 || n_tokens > OLED_MAX_ROUTE_TOKENS || one_launch(n_tokens, routing->top_k)) return 0;
-  return (size_t)scored_parts(n_tokens) * (size_t)routing->n_experts * sizeof(int32_t);
+  return (size_t)scored_parts(n_tokens) * (size_t)hist_stride(routing->n_experts) * sizeof(uint16_t) + 4;  // (+ 4: on 8-byte boundaries)
 }
 
 extern "C" int oled_route_scored(const oled_routing* routing, const float* logits, int64_t logits_stride, const float* bias,
@@ -936,14 +967,14 @@ extern "C" int oled_route_scored(const oled_routing* routing, const float* logit
   } else {
     a.parts = scored_parts(T);
     a.part_tokens = (T + a.parts - 1) / a.parts;
-    if (order) a.hist = static_cast<int32_t*>(scratch);
+    if (order) a.hist = reinterpret_cast<uint16_t*>((reinterpret_cast<uintptr_t>(scratch) + 7) & ~(uintptr_t)7);
+    a.hist_stride = hist_stride(E);
     err = launch_scored(st, a, a.parts);
-    // (each of these indexes by what the one before has stored: it is launched only behind one that was)
+    // (it indexes by what the routing has stored: it is launched only behind one that was)
+    if (err == cudaSuccess && order) err = cudaFuncSetAttribute(place_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPlaceSmem);
     if (err == cudaSuccess && order)
-      err = launch_pdl(scan_hist_kernel, dim3((unsigned)((E + 7) / 8)), dim3(256), 0, st, a.hist, a.parts, E, counts);
-    if (err == cudaSuccess && order)
-      err = launch_pdl(place_kernel, dim3((unsigned)a.parts), dim3(kScoredThreads), (size_t)kScoredWarps * E * sizeof(int), st,
-                       (const int32_t*)ids, T, K, E, a.part_tokens, (const int32_t*)a.hist, (const int32_t*)counts, offsets, perm);
+      err = launch_pdl(place_kernel, dim3((unsigned)a.parts), dim3(kScoredThreads), kPlaceSmem, st,
+                       (const int32_t*)ids, T, K, E, a.part_tokens, (const uint16_t*)a.hist, a.hist_stride, counts, offsets, perm);
   }
   return cudaGetLastError() == cudaSuccess && err == cudaSuccess ? OLED_OK : OLED_ERR_CUDA;
 }
