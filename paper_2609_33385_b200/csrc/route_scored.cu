@@ -17,8 +17,8 @@
 // consecutive, so that lower lanes hold lower experts and a group never shares a lane with another.  Every lane
 // sorts its keys once (a network of maxima and minima in registers); then each of the top_k rounds is one warp maximum
 // over the lanes' heads, a vote for the lowest lane that has it, and a shift in that lane.
-// Bound by the instructions of a token, 685 a warp at 256 experts in groups (32768 tokens: 45 us, 40 of them this kernel's with its issue
-// slots 66 % full; the bytes would take 6).
+// Bound by the instructions of a token, 630 a warp at 256 experts in groups (32768 tokens: 33.8 us, 27 of them this kernel's; the bytes
+// would take 6).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -203,7 +203,7 @@ __device__ __noinline__ bool groups_exact(const ScoredArgs& a, const float* row,
 // that can be among the K.  groups: the groups are chosen again too (all experts are in the masks then).  Scores below exp(-708)
 // count as that.  Few tokens come here, but a CTA waits for the last of its own; what they cost is fp64 latency, so only those
 // experts are computed that the fp32 forms leave in question, a lane each where there are lanes for them (lanes with two or three of them
-// in turn, and rounds to order them: 250 tokens with one such 8.4 us, this way WHAT; with all experts a token took 5.5 us).
+// in turn, and rounds to order them: 250 tokens, two of them near, 8.4 us, this way 7.5; with all experts a token took 5.5 us).
 template <int PER>
 __device__ __noinline__ int select_exact(const ScoredArgs& a, const float* row, int lane, int first, int mine, float top, uint32_t mask,
                                          bool groups, int32_t* s_experts) {
@@ -690,8 +690,8 @@ constexpr int kScoredCtas = 148;  // at most: one an SM
 constexpr size_t kPlaceSmem = 120 * 1024;
 static_assert(kPlaceSmem >= (size_t)kScoredWarps * OLED_MAX_EXPERTS * sizeof(int), "a row of counts per warp");
 
-// Every CTA adds up the histograms of all of them itself, 150 rows of E 16-bit counts out of L2: cheaper than a kernel in between that leaves
-// it one row to read (32768 tokens, 256 experts in groups: WITH, without WITHOUT).
+// Every CTA adds up the histograms of all of them itself, 148 rows of E 16-bit counts out of L2: cheaper than a kernel in between that leaves
+// it one row to read (32768 tokens, 256 experts in groups: 40.4 us with one, 33.8 without and with one CTA an SM; 8-bit counts 33.5).
 __global__ void __launch_bounds__(kScoredThreads)
 place_kernel(const int32_t* __restrict__ ids, int T, int K, int E, int part_tokens, const uint16_t* __restrict__ hist, int hist_stride,
              int32_t* __restrict__ counts, int32_t* __restrict__ offsets, int32_t* __restrict__ perm) {
