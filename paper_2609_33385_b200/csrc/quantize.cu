@@ -44,7 +44,8 @@ quantize_kernel(const uint16_t* __restrict__ x, int64_t x_stride, int64_t pieces
       float v[8], u[8];
       unpack8(a[i], v);
       unpack8(b[i], u);
-      // (the sigmoid's fast exponential and quotient are off by some 2^-21, the code by 2^-4)
+      // (The sigmoid's fast exponential and quotient are off by some 2^-21, the code by 2^-4: of 6.3 M codes 19 are on the other side of a rounding's
+      // border from 64 bits, with expf() 17 and 8192 x 4096 in 35.0 us instead of 28.7, with an IEEE quotient too 12 and 42.8.)
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = __fdividef(v[j], 1.0f + __expf(-v[j])) * u[j];
       const uint32_t amax = amax_half_warp(amax8(v));

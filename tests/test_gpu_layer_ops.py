@@ -175,6 +175,52 @@ def test_route_groups_whose_border_fp32_cannot_tell(b, score, e, groups, top_gro
             check_route(b, logits, bias, top_k=k, score=score, n_groups=groups, top_groups=top_groups, group_top=group_top)
 
 
+@pytest.mark.parametrize("t,e,k", [(4500, 1, 1), (4111, 2, 1), (2500, 3, 2), (1200, 7, 7), (900, 13, 5), (700, 40, 17), (150, 510, 32), (129, 512, 32), (40001, 9, 1), (1 << 20, 5, 2)])
+def test_route_order_of_many_assignments(b, t, e, k):
+    """The order of more assignments than one launch takes: few and odd numbers of experts, tokens that do not fill the CTAs."""
+    gen = torch.Generator(device=DEV).manual_seed(t)
+    logits = torch.randn((t, e), device=DEV, generator=gen)
+    r = b.Routing(e, k)
+    ids, gate = torch.empty((t, k), dtype=torch.int32, device=DEV), torch.empty((t, k), device=DEV)
+    counts, offsets = torch.full((e + 1,), -7, dtype=torch.int32, device=DEV), torch.full((e + 2,), -7, dtype=torch.int32, device=DEV)
+    perm = torch.full((t * k + 1,), -7, dtype=torch.int32, device=DEV)
+    need = b.route_scored_scratch(r, t)
+    for shift in (0, 1):  # scratch on 8-byte boundaries, and on 4-byte ones alone
+        scratch = torch.full((need // 4 + 3,), -7, dtype=torch.int32, device=DEV)
+        ok(b, b.route_scored(r, logits.data_ptr(), e, None, t, stream(), ids.data_ptr(), gate.data_ptr(), counts.data_ptr(), offsets.data_ptr(), perm.data_ptr(),
+                             scratch.data_ptr() + 4 * shift, need))
+        torch.cuda.synchronize()
+        assert bool((scratch[shift + need // 4:] == -7).all()) and bool((scratch[:shift] == -7).all())
+        expected = torch.sort(logits.double(), dim=1, descending=True, stable=True).indices[:, :k]
+        assert bool((ids == expected).all())
+        flat = ids.flatten().long()
+        assert bool((perm[:-1] == torch.sort(flat, stable=True).indices).all()) and int(perm[-1]) == -7
+        n = torch.bincount(flat, minlength=e)
+        assert bool((counts[:e] == n).all()) and int(counts[e]) == -7
+        assert bool((offsets[1:e + 1] == torch.cumsum(n, 0)).all()) and int(offsets[0]) == 0 and int(offsets[e + 1]) == -7
+
+
+@pytest.mark.parametrize("score", [0, 1])
+def test_route_with_fewer_finite_choices_than_wanted(b, score):
+    """Groups that stay and have fewer experts than wanted that are not at -inf, by their logits or by their bias."""
+    rng = np.random.default_rng(10)
+    t, e, groups = 90, 48, 4
+    logits = rng.normal(size=(t, e)).astype(np.float32)
+    for i in range(t):
+        for g in range(groups):
+            keep = rng.choice(12, rng.integers(0 if i % 3 == 0 else 1, 5), replace=False)
+            gone = np.setdiff1d(np.arange(12), keep)
+            logits[i, g * 12 + gone] = -np.inf
+    masked = np.where(np.arange(e) % 12 < 2, 0.1, -np.inf).astype(np.float32)
+    finite = rng.normal(size=(t, e)).astype(np.float32)
+    for group_top in (1, 2):
+        for top_groups in (2, 3):
+            check_route(b, logits, None, top_k=7, score=score, n_groups=groups, top_groups=top_groups, group_top=group_top)
+            check_route(b, finite, masked, top_k=7, score=score, n_groups=groups, top_groups=top_groups, group_top=group_top)
+    check_route(b, logits, None, top_k=9, score=score)
+    check_route(b, finite, masked, top_k=9, score=score)
+
+
 @pytest.mark.parametrize("score", [0, 1])
 def test_route_non_finite(b, score):
     rng = np.random.default_rng(6)
