@@ -387,7 +387,7 @@ int oled_route_noalloc(const void* hidden, const void* w_router, const float* bi
  *   groups consecutive experts; a group counts as its largest choice (group_top 1) or as the sum of its two largest
  *          s_e + bias_e (2), and the token's experts come from the top_groups largest groups.
  *   ids    the top_k largest choices, in descending order.  Equal values go to the lower index.  Choices are told apart as
- *          in 64-bit arithmetic, whatever the speed of the scores' own precision would suggest.
+ *          64-bit arithmetic tells them apart, also where fp32 scores are equal.
  *   gate   scale * s / (sum of the chosen s + 1e-20) with renormalise, else scale * s.
  * A NaN logit counts as -inf, its choice and a choice that is NaN too; the ids of a token stay distinct, also where every
  * choice is -inf. */
