@@ -516,8 +516,9 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
     int at = 0;
     const float before = __shfl_up_sync(0xffffffffu, my_key, 1);
     if (!__any_sync(0xffffffffu, lane > 0 && lane < a.K && before == my_key)) {
+      // (downwards: of equal keys of the lane, one of them chosen and one not, the first counts)
 #pragma unroll
-      for (int i = 1; i < PER; ++i) at = __shfl_sync(0xffffffffu, key[i], my_lane) == my_key ? i : at;
+      for (int i = PER - 1; i >= 0; --i) at = __shfl_sync(0xffffffffu, key[i], my_lane) == my_key ? i : at;
     } else {  // equal keys of one lane are taken in the order of their indices
       const uint32_t same = __match_any_sync(0xffffffffu, __float_as_uint(__fadd_rn(my_key, 0.0f))) & __match_any_sync(0xffffffffu, my_lane);
       int skip = __popc(same & ((1u << lane) - 1u));

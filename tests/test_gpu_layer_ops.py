@@ -655,3 +655,35 @@ def test_products_on_two_streams(b):
     for o in outs:
         for got, ref in zip(o, want):
             assert torch.equal(got.view(torch.int16), ref.view(torch.int16))
+
+
+def border_ties(e, k, rng, pairs):
+    """Logits of a token per pair (a, b): the K-1 largest are distinct, the two next are equal and at a and b, the others are distinct and lower."""
+    t = len(pairs)
+    logits = -1 - 0.001 * np.argsort(rng.random((t, e)), axis=1).astype(np.float32)
+    for i, (x, y) in enumerate(pairs):
+        others = rng.permutation(np.setdiff1d(np.arange(e), (x, y)))[:k - 1]
+        logits[i, others] = 1 + 0.01 * np.arange(k - 1, dtype=np.float32)
+        logits[i, [x, y]] = 0.5
+    return logits
+
+
+@pytest.mark.parametrize("k", [1, 8])
+@pytest.mark.parametrize("e,groups,top_groups", [(40, 1, 1), (64, 1, 1), (128, 1, 1), (160, 1, 1), (256, 1, 1), (384, 1, 1), (512, 1, 1), (96, 3, 2), (256, 8, 4), (512, 16, 9), (504, 18, 9), (512, 32, 20)])
+def test_route_ties_between_the_last_choice_and_the_next_one(b, e, groups, top_groups, k):
+    """Without a bias, equal logits of which one is the K-th choice: the lower index has it, wherever the two lie."""
+    rng = np.random.default_rng(11)
+    near = [(x, x + 1) for x in range(e - 1)]                                  # (mostly of one lane)
+    far = [tuple(sorted(rng.choice(e, 2, replace=False))) for _ in range(100)]
+    logits = border_ties(e, k, rng, near + far)
+    for group_top in (1, 2):
+        for score in (0, 1):
+            check_route(b, logits, None, top_k=k, score=score, n_groups=groups, top_groups=top_groups, group_top=group_top)
+
+
+@pytest.mark.parametrize("e,groups,top_groups", [(64, 1, 1), (256, 1, 1), (512, 1, 1), (256, 8, 4), (504, 18, 9)])
+def test_route_logits_that_were_bf16(b, e, groups, top_groups):
+    """Logits of a bf16 gate: equal ones are common, and some of them lie at the border of the choice."""
+    logits = torch.randn(3000, e, generator=torch.Generator().manual_seed(e)).to(torch.bfloat16).float().numpy()
+    for score, group_top in ((0, 1), (1, 2)):
+        check_route(b, logits, None, top_k=8, score=score, n_groups=groups, top_groups=top_groups, group_top=group_top)
