@@ -93,11 +93,12 @@ __device__ __forceinline__ unsigned long long order_key64(double v) {  // v is n
   return (bits >> 63) ? ~bits : (bits | 0x8000000000000000ull);
 }
 
-// exp(x) in fp64 for |x| <= 708 (clamped beyond), without a branch so that several run side by side: x = n ln 2 + r with ln 2 in two
-// parts (Cody and Waite), the Taylor polynomial of degree 13 for |r| <= ln 2 / 2 (its remainder is below 2^-57 of the
-// result), and n added to the exponent.  Off by a few units in the last place.
+// exp(x) in fp64, without a branch so that several run side by side: x = n ln 2 + r with ln 2 in two parts (Cody and Waite), the
+// Taylor polynomial of degree 13 for |r| <= ln 2 / 2 (its remainder is below 2^-57 of the result), and 2^n in two factors, so that
+// results down to the smallest subnormal number are rounded once, and zero and infinity beyond them come by themselves.  Off by a few
+// units in the last place.
 __device__ __forceinline__ double exp_double(double x) {
-  x = fmin(fmax(x, -708.0), 708.0);
+  x = fmin(fmax(x, -746.0), 710.0);  // (exp(-746) < 2^-1075, exp(710) > 2^1024)
   const double n = rint(x * 1.4426950408889634074);
   double r = fma(-n, 6.93147180369123816490e-01, x);  // ln 2 without its low 21 bits: n times it is exact
   r = fma(-n, 1.90821492927058770002e-10, r);
@@ -115,9 +116,10 @@ __device__ __forceinline__ double exp_double(double x) {
   p = fma(p, r, 0.5);
   p = fma(p, r, 1.0);
   p = fma(p, r, 1.0);
-  return __longlong_as_double(__double_as_longlong(p) + ((long long)(int)n << 52));
+  const int whole = (int)n, half = whole / 2;
+  return __longlong_as_double(__double_as_longlong(p) + ((long long)half << 52)) * __longlong_as_double((long long)(1023 + whole - half) << 52);
 }
-// 1 / x for normal x, by Newton's iteration from an approximation of 2^-20.
+// 1 / x for x of 1 to 2^1000, by Newton's iteration from an approximation of 2^-20.
 __device__ __forceinline__ double reciprocal_double(double x) {
   double y;
   asm("rcp.approx.ftz.f64 %0, %1;" : "=d"(y) : "d"(x));
@@ -141,7 +143,9 @@ __device__ __forceinline__ double sum_exact(const float* row, int first, int min
 __device__ __forceinline__ double choice_exact(const ScoredArgs& a, const float* row, int e, float top, double sum, double& score) {
   const float l = row[e], x = no_nan(l);
   const double ex = exp_double(a.softmax ? (x == top ? 0.0 : (double)x - (double)top) : -(double)x);
-  score = (a.softmax ? ex : 1.0) * reciprocal_double(a.softmax ? sum : 1.0 + ex);
+  const double num = a.softmax ? ex : 1.0, den = a.softmax ? sum : 1.0 + ex;
+  // (next to the smallest numbers the quotient is rounded once)
+  score = num < 0x1p-900 || den > 0x1p900 ? num / den : num * reciprocal_double(den);
   const double c = a.bias == nullptr ? (double)l : score + (double)a.bias[e];
   return l == l && c == c ? c : -INFINITY;
 }
@@ -200,8 +204,8 @@ __device__ __noinline__ bool groups_exact(const ScoredArgs& a, const float* row,
 }
 
 // The choice of one token in fp64, by the warp that holds its logits: lane r < K ends with the id of rank r.  mask: the lane's experts
-// that can be among the K.  groups: the groups are chosen again too (all experts are in the masks then).  Scores below exp(-708)
-// count as that.  Few tokens come here, but a CTA waits for the last of its own; what they cost is fp64 latency, so only those
+// that can be among the K.  groups: the groups are chosen again too (all experts are in the masks then).
+// Few tokens come here, but a CTA waits for the last of its own; what they cost is fp64 latency, so only those
 // experts are computed that the fp32 forms leave in question, a lane each where there are lanes for them (lanes with two or three of them
 // in turn, and rounds to order them: 250 tokens, two of them near, 8.4 us, this way 7.5; with all experts a token took 5.5 us).
 template <int PER>

@@ -687,3 +687,19 @@ def test_route_logits_that_were_bf16(b, e, groups, top_groups):
     logits = torch.randn(3000, e, generator=torch.Generator().manual_seed(e)).to(torch.bfloat16).float().numpy()
     for score, group_top in ((0, 1), (1, 2)):
         check_route(b, logits, None, top_k=8, score=score, n_groups=groups, top_groups=top_groups, group_top=group_top)
+
+
+@pytest.mark.parametrize("score", [0, 1])
+def test_route_choices_next_to_the_smallest_numbers(b, score):
+    """Scores that only the range of 64-bit numbers tells apart, down to its smallest ones, beside a bias that does not cover them."""
+    check_route(b, np.float32([[0, -740, -720, -800]]), np.zeros(4, np.float32), top_k=3, score=score)
+    rng = np.random.default_rng(12)
+    for e, groups, top_groups in ((24, 1, 1), (64, 1, 1), (256, 1, 1), (64, 4, 2), (256, 8, 3)):
+        logits = rng.uniform(-755, -690, size=(60, e)).astype(np.float32)
+        logits[::3] = rng.uniform(-755, -80, size=(20, e)).astype(np.float32)
+        logits[np.arange(60), rng.integers(0, e, 60)] = 0.0 if score == 0 else -690.0
+        for bias in (np.zeros(e, np.float32), np.where(np.arange(e) % 3 == 0, -np.inf, 0).astype(np.float32)):
+            for group_top in (1, 2):
+                check_route(b, logits, bias, top_k=min(e // 2, 12), score=score, n_groups=groups, top_groups=top_groups, group_top=group_top, renormalise=0)
+        for group_top in (1, 2):  # without a bias the two largest scores of a group are added all the same
+            check_route(b, logits, None, top_k=min(e // 2, 12), score=score, n_groups=groups, top_groups=top_groups, group_top=group_top, renormalise=0)
