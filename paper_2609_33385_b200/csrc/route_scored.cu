@@ -403,6 +403,7 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
       t1 = fmaxf(t1, o1);
     }
     float group_slack = slack;
+    float off = 0.0f;  // what the group's fp32 value is off by at most, the scores' part apart
     const float least = a.group_top == 2 ? t2 : t1;  // what an expert has to reach to count for its group
     if (a.group_top == 2) {
       if (a.bias == nullptr) {  // the order of scores is that of logits
@@ -416,7 +417,11 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
           group_slack = 5.8e-7f;
         }
       }
+      // two choices and their sum, each rounded: 2^-24 of the larger choice twice, and of the sum, which is twice that at most or, where
+      // the two cancel, nearly nothing
+      if (a.bias != nullptr) off = 2.4e-7f * fmaxf(fabsf(t1), fabsf(t2));
       t1 += t2;
+      if (!(fabsf(t1) <= 3.4028235e38f)) off = 0.0f;
       group_slack *= 2.0f;
     }
     // rounds over the groups: the lanes of the largest value drop out
@@ -428,8 +433,10 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
       last = reduce_max(left);
       left = left == last ? kNone : left;
     }
-    const float next = reduce_max(left);  // (every lane takes part, so not behind a condition of its own)
     keep = g < a.G && value >= last;
+    // (every lane takes part in these, so not behind conditions of its own)
+    const float next = reduce_max(keep || g >= a.G ? kNone : value + off);  // as much as a group that goes may be
+    if (a.bias != nullptr && a.group_top == 2) last = last == kNone ? kNone : -reduce_max(keep ? off - value : kNone);  // as little as one that stays may be
     if (last == kNone) {
       near_group = true;
     } else if (__popc(__ballot_sync(0xffffffffu, keep)) != a.top_groups << a.lanes_log2) {  // equal values: the lower groups
@@ -443,8 +450,8 @@ __device__ __forceinline__ void route_token(const ScoredArgs& a, int t, int lane
       keep = g < a.G && before < a.top_groups;
     } else if ((a.bias != nullptr || a.group_top == 2) && near_choices(last, next, group_slack)) {
       // Groups clearly above the best one that goes stay, groups clearly below the least one that stays go; between the others ...
-      const bool sure = keep && !near_choices(value, next, group_slack);
-      const bool question = g < a.G && !sure && (keep || near_choices(last, value, group_slack));
+      const bool sure = keep && !near_choices(value - off, next, group_slack);
+      const bool question = g < a.G && !sure && (keep || near_choices(last, value + off, group_slack));
       uint32_t mask = 0u;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {

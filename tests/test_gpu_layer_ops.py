@@ -703,3 +703,19 @@ def test_route_choices_next_to_the_smallest_numbers(b, score):
                 check_route(b, logits, bias, top_k=min(e // 2, 12), score=score, n_groups=groups, top_groups=top_groups, group_top=group_top, renormalise=0)
         for group_top in (1, 2):  # without a bias the two largest scores of a group are added all the same
             check_route(b, logits, None, top_k=min(e // 2, 12), score=score, n_groups=groups, top_groups=top_groups, group_top=group_top, renormalise=0)
+
+
+@pytest.mark.parametrize("score", [0, 1])
+@pytest.mark.parametrize("size,groups,top_groups", [(4, 8, 3), (8, 8, 4), (2, 32, 9), (16, 3, 1)])
+def test_route_groups_whose_two_choices_cancel(b, score, size, groups, top_groups):
+    """The two largest choices of a group are far larger than their sum, so that their fp32 forms are off by more than the sums are apart."""
+    rng = np.random.default_rng(13)
+    t, e = 150, size * groups
+    for big in (10.0, 100.0, 3e4):
+        bias = np.full((groups, size), -8 * big, np.float32)
+        bias[:, 0], bias[:, 1] = big, -big
+        bias = np.stack([rng.permutation(r) for r in bias]).reshape(-1)
+        logits = rng.normal(size=(t, 1, 1)) + np.zeros((t, groups, size))
+        logits = logits + rng.uniform(-1, 1, size=logits.shape) * (2.0 ** -rng.integers(4, 24, size=(t, 1, 1)))  # sums apart by 1e-7 to 0.1
+        check_route(b, logits.reshape(t, e).astype(np.float32), bias, top_k=min(top_groups * size, 4), score=score, n_groups=groups, top_groups=top_groups,
+                    group_top=2)
