@@ -297,14 +297,16 @@ int oled_get_capacity(oled_ctx* ctx, int32_t* capacity);
 /* Per-kernel timing collected while OLED_OPT_PROFILE is on.  bytes / flops are the ALGORITHMIC
  * figures of the launches (weights of each expert once, token rows in, result rows out), not
  * measured traffic. */
-#define OLED_KERNEL_ROUTE 0
+#define OLED_KERNEL_ROUTE 0 /* with a registered routing two launches: logits, choice */
 #define OLED_KERNEL_PERMUTE 1
 #define OLED_KERNEL_GATHER 2
 #define OLED_KERNEL_FFN_GATE_UP 3
 #define OLED_KERNEL_FFN_DOWN 4
 #define OLED_KERNEL_COMBINE 5
 #define OLED_KERNEL_FFN_FUSED 6 /* gate/up + SwiGLU + down projection in one launch */
-#define OLED_N_KERNELS 7
+#define OLED_KERNEL_SHARED_EXPERT 7 /* a shared expert's quantisations and products: four launches */
+#define OLED_KERNEL_NORM 8          /* the norms between an iteration's layers */
+#define OLED_N_KERNELS 9
 typedef struct {
   uint64_t launches;
   double ms;       /* sum of CUDA-event durations */

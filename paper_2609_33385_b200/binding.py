@@ -35,7 +35,7 @@ CHECK_FLAGS = {0x01: "id_range", 0x02: "id_duplicate", 0x04: "offsets", 0x08: "p
                0x20: "row_expert", 0x40: "order"}
 POLICY_PRIORITY, POLICY_LRU, POLICY_LFU = 0, 1, 2
 POLICY_IDS = {"priority": 0, "lru": 1, "lfu": 2}
-KERNEL_NAMES = ["route", "permute", "gather", "ffn_gate_up", "ffn_down", "combine", "ffn_fused"]
+KERNEL_NAMES = ["route", "permute", "gather", "ffn_gate_up", "ffn_down", "combine", "ffn_fused", "shared_expert", "norm"]
 
 EXPORTS = [
     "oled_create", "oled_register_router", "oled_register_experts", "oled_denoise_step",

@@ -803,13 +803,23 @@ int oled_register_shared_expert(oled_ctx* ctx, int32_t layer, const oled_shared_
 static int shared_expert_up(oled_ctx* ctx, const LayerData& L, const void* hidden, int T) {
   NvtxRange nv(ctx, "oled.step.shared_expert_up");
   const int H = ctx->shape.hidden, I = L.shared.intermediate;
-  OLED_CUDA(ctx, launch_quantize(ctx->stream, static_cast<const uint16_t*>(hidden), H, T, H, false, ctx->d_shared_codes, H, ctx->d_shared_scales,
-                                 H / 128));
-  oled_product_shape up{2 * I, H, OLED_BF16, H, H / 128, H, H / 128, 0, 2 * I};
-  const int rc = matmul_blocks(&up, ctx->d_shared_codes, ctx->d_shared_scales, L.shared.gate_up, L.shared.gate_up_scale, nullptr, T, ctx->stream,
-                               ctx->d_shared_mid);
-  if (rc != OLED_OK) return rc;
-  OLED_CUDA(ctx, launch_quantize(ctx->stream, ctx->d_shared_mid, 2 * I, T, I, true, ctx->d_shared_act, I, ctx->d_shared_act_scales, I / 128));
+  const uint64_t t = T, h = H, i = I;
+  {
+    ProfScope ps(ctx, OLED_KERNEL_SHARED_EXPERT, t * h * 3 + t * h / 32, 4 * t * h);
+    OLED_CUDA(ctx, launch_quantize(ctx->stream, static_cast<const uint16_t*>(hidden), H, T, H, false, ctx->d_shared_codes, H, ctx->d_shared_scales,
+                                   H / 128));
+  }
+  {
+    ProfScope ps(ctx, OLED_KERNEL_SHARED_EXPERT, t * h + t * h / 32 + 2 * i * h + t * 4 * i, 4 * t * i * h);
+    oled_product_shape up{2 * I, H, OLED_BF16, H, H / 128, H, H / 128, 0, 2 * I};
+    const int rc = matmul_blocks(&up, ctx->d_shared_codes, ctx->d_shared_scales, L.shared.gate_up, L.shared.gate_up_scale, nullptr, T, ctx->stream,
+                                 ctx->d_shared_mid);
+    if (rc != OLED_OK) return rc;
+  }
+  {
+    ProfScope ps(ctx, OLED_KERNEL_SHARED_EXPERT, t * i * 5 + t * i / 32, 12 * t * i);
+    OLED_CUDA(ctx, launch_quantize(ctx->stream, ctx->d_shared_mid, 2 * I, T, I, true, ctx->d_shared_act, I, ctx->d_shared_act_scales, I / 128));
+  }
   ctx->launches += 3;
   return OLED_OK;
 }
@@ -818,6 +828,8 @@ static int shared_expert_up(oled_ctx* ctx, const LayerData& L, const void* hidde
 static int shared_expert_down(oled_ctx* ctx, const LayerData& L, int T, void* out) {
   NvtxRange nv(ctx, "oled.step.shared_expert_down");
   const int H = ctx->shape.hidden, I = L.shared.intermediate;
+  const uint64_t t = T, h = H, i = I;
+  ProfScope ps(ctx, OLED_KERNEL_SHARED_EXPERT, t * i + t * i / 32 + i * h + t * h * 4, 2 * t * i * h);
   oled_product_shape down{H, I, OLED_BF16, I, I / 128, I, I / 128, H, H};
   const int rc = matmul_blocks(&down, ctx->d_shared_act, ctx->d_shared_act_scales, L.shared.down, L.shared.down_scale, out, T, ctx->stream, out);
   ctx->launches += 1;
@@ -937,11 +949,13 @@ static int step_impl(oled_ctx* ctx, int32_t layer, const void* hidden, const flo
     launch_route(st, static_cast<const uint16_t*>(hidden), L.w_router, L.bias, confidences, T, H, E, K,
                  ctx->d_logits, ctx->d_ids, ctx->d_gate, ctx->d_counts, ctx->d_scores, prev, tl, seg_counts, seg_tokens,
                  ctx->scatter, L.scored);
-    if (L.scored) {
-      OLED_CUDA(ctx, launch_route_step(st, L.routing, ctx->d_logits, L.has_score_bias ? L.score_bias : nullptr, confidences, T, ctx->d_ids,
-                                       ctx->d_gate, ctx->d_counts, ctx->d_scores, seg_counts, seg_tokens));
-      ctx->launches += 1;
-    }
+  }
+  if (L.scored) {
+    NvtxRange nv(ctx, "oled.step.1_scored_routing");
+    ProfScope ps(ctx, OLED_KERNEL_ROUTE, (uint64_t)T * E * 4 + (uint64_t)T * K * 8, 12ull * T * E);
+    OLED_CUDA(ctx, launch_route_step(st, L.routing, ctx->d_logits, L.has_score_bias ? L.score_bias : nullptr, confidences, T, ctx->d_ids,
+                                     ctx->d_gate, ctx->d_counts, ctx->d_scores, seg_counts, seg_tokens));
+    ctx->launches += 1;
   }
   // Many rows per expert (every FFN launch of the step on CTA pairs, token tiles of 256 rows): no
   // gather kernel, each gate/up launch copies its experts' token rows while its first items run.
@@ -1143,6 +1157,7 @@ static int step_impl(oled_ctx* ctx, int32_t layer, const void* hidden, const flo
       const int rcs = shared_expert_down(ctx, L, T, out);
       if (rcs != OLED_OK) return rcs;
       if (x_next != nullptr) {
+        ProfScope ps(ctx, OLED_KERNEL_COMBINE, (uint64_t)T * H * 6, (uint64_t)T * H);
         launch_residual_add(st, static_cast<const uint16_t*>(hidden), static_cast<const uint16_t*>(out), static_cast<uint16_t*>(x_next),
                             (size_t)T * H);
         ctx->launches += 1;
@@ -1262,6 +1277,9 @@ static int norm_between(oled_ctx* ctx, const LayerData* done, const LayerData* n
     post = done->norms.post_weight;
     gate = done->norms.gate;
   }
+  NvtxRange nv(ctx, "oled.iteration.norms");
+  ProfScope ps(ctx, OLED_KERNEL_NORM, (uint64_t)n_tokens * H * 2 * (1 + (y != nullptr) + (x_out != nullptr) + (next != nullptr)),
+               10ull * n_tokens * H);
   const int rc = norm_residual(&s, x, y, post, gate, next ? next->norms.pre_weight : nullptr, n_tokens, ctx->stream, x_out,
                                next ? ctx->d_norm : nullptr, nullptr, nullptr, next ? next->norms.eps : 0.0f);
   ctx->launches += 1;

@@ -313,3 +313,44 @@ def test_registrations_refuse(b):
         assert np.array_equal(got["ids"], om.topk_route(ctx.debug_logits(0, 8), 2)[0])
     finally:
         run.close()
+
+
+@pytest.mark.parametrize("n", [4, 300])
+def test_profile_counts_what_stands_around_the_layers(b, n):
+    """Every launch of an iteration with routing, norms and shared experts is in the profile, under its own name."""
+    h, layers = 256, 2
+    w = synth.tiny(n_layers=layers, n_experts=16, top_k=3, hidden=h, intermediate=256)
+    run = runner(w, capacity=[16, 16], max_tokens=n)
+    try:
+        keep, desc = shared_expert(b, h, 128, 9)
+        ones = torch.ones(h, dtype=torch.bfloat16, device="cuda:0")
+        h_bits, conf = synth.flat_tokens(w, n, 1)
+        x, c = dev(h_bits), torch.from_numpy(conf).cuda()
+        got = torch.empty_like(x)
+
+        def launched():
+            run.ctx.denoise_iteration(x.data_ptr(), c.data_ptr(), n, got.data_ptr())   # (fetches what it misses)
+            run.ctx.synchronize()
+            run.ctx.profile_read()
+            before = run.ctx.launch_count()
+            run.ctx.denoise_iteration(x.data_ptr(), c.data_ptr(), n, got.data_ptr())
+            count = run.ctx.launch_count() - before
+            prof = run.ctx.profile_read()
+            assert all(p["ms"] > 0 and p["bytes"] > 0 for p in prof.values() if p["launches"])
+            return count, {k: p["launches"] for k, p in prof.items()}
+
+        run.ctx.set_option(b.OPT_PROFILE, 1)
+        count, plain = launched()
+        assert plain["shared_expert"] == plain["norm"] == 0 and plain["route"] == layers and sum(plain.values()) == count
+        for layer in range(layers):
+            run.ctx.register_shared_expert(layer, desc)
+            run.ctx.register_routing(layer, b.Routing(16, 3, score=b.SCORE_SIGMOID))
+        count, prof = launched()
+        assert prof["shared_expert"] == 4 * layers and prof["norm"] == 0 and prof["route"] == 2 * layers and prof["combine"] == 2 * layers
+        assert sum(prof.values()) == count
+        for layer in range(layers):
+            run.ctx.register_norms(layer, b.LayerNorms(ones.data_ptr(), ones.data_ptr(), None, 0, 1e-6, 1.0))
+        count, prof = launched()
+        assert prof["shared_expert"] == 4 * layers and prof["norm"] == layers + 1 and prof["combine"] == layers and sum(prof.values()) == count
+    finally:
+        run.close()
