@@ -329,8 +329,11 @@ product_few_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_const
 
 // ---- many rows of A: pairs of CTAs -------------------------------------------------------------
 constexpr int kManyEpiWarps = 8, kManyProducer = 8, kManyMma = 9, kManyThreads = 12 * 32;
-// Registers a thread: 168 at launch (12 warps), of which the third warpgroup gives to the two that accumulate: 4 x 56 + 8 x 224 = 12 x 168.
-constexpr int kManyFewRegs = 56, kManyEpiRegs = 224;
+// Registers a thread: 168 at launch (12 warps), of which the third warpgroup gives to the two that accumulate.
+constexpr int kManyRegs = 168, kManyFewRegs = 56, kManyEpiRegs = 224;
+static_assert(4 * kManyFewRegs + 8 * kManyEpiRegs == 12 * kManyRegs, "what one warpgroup gives the others take");
+// An SM has 65536: beside a CTA of this kernel there is room for 1024, less than any CTA takes that uses tensor memory (six warps and more).
+static_assert(65536 - kManyThreads * kManyRegs < 6 * 32 * 16, "no second CTA with tensor memory on the SM");
 constexpr int kManyStages = 4, kManyRows = 256, kManyCols = 256;  // of a pair's tile
 constexpr uint32_t kManyStage = 2 * kWTile;
 constexpr uint32_t kManyOut = 8192;  // staging of a warp's results: 32 rows x 128 bytes, twice
@@ -381,7 +384,10 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_cons
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_a)) : "memory");
   }
   griddep_wait();
-  if (warp == kManyMma) {  // (all of it: no other kernel that takes tensor memory fits beside this one's shared memory)
+  // All of tensor memory: the registers leave no room on the SM for another CTA that takes any (shared memory would: product_few_kernel<16>
+  // with one k-block needs 29 KB).  Were there one, it would be waited for and not the other way round: whoever holds tensor memory gives it
+  // back without waiting for another kernel.
+  if (warp == kManyMma) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(512)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");

@@ -719,3 +719,29 @@ def test_route_groups_whose_two_choices_cancel(b, score, size, groups, top_group
         logits = logits + rng.uniform(-1, 1, size=logits.shape) * (2.0 ** -rng.integers(4, 24, size=(t, 1, 1)))  # sums apart by 1e-7 to 0.1
         check_route(b, logits.reshape(t, e).astype(np.float32), bias, top_k=min(top_groups * size, 4), score=score, n_groups=groups, top_groups=top_groups,
                     group_top=2)
+
+
+def test_products_on_pairs_beside_others(b):
+    """Launches on pairs of CTAs in several streams, next to one another and to the smallest calls: they share nothing, tensor memory apart."""
+    shapes = [(2304, 2048, 1024), (1, 128, 128), (16, 4096, 128), (1300, 4096, 384), (9, 2048, 512)]
+    sets = []
+    for m, n, k in shapes:
+        a, sa, w, sb = (t.to(DEV) for t in product_inputs(m, n, k))
+        shape = b.ProductShape(n=n, k=k, out=0, a_stride=k, a_scale_stride=sa.shape[1], b_stride=k, b_scale_stride=sa.shape[1], add_stride=0, out_stride=n)
+        sets.append((shape, a, sa, w, sb, m, torch.empty((m, n), dtype=torch.bfloat16, device=DEV)))
+    want = []
+    for shape, a, sa, w, sb, m, out in sets:
+        ok(b, b.matmul_blocks(shape, ptr(a), ptr(sa), ptr(w), ptr(sb), None, m, stream(), ptr(out)))
+        want.append(out.clone())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    outs = [[torch.full_like(s[6], 7.0) for s in sets] for _ in streams]
+    for r in range(40):
+        for i, (st, o) in enumerate(zip(streams, outs)):
+            for j in range(len(sets)):  # (each stream begins with another shape)
+                shape, a, sa, w, sb, m, _ = sets[(i + j) % len(sets)]
+                ok(b, b.matmul_blocks(shape, ptr(a), ptr(sa), ptr(w), ptr(sb), None, m, st.cuda_stream, ptr(o[(i + j) % len(sets)])))
+    torch.cuda.synchronize()
+    for o in outs:
+        for got, ref in zip(o, want):
+            assert torch.equal(got.view(torch.int16), ref.view(torch.int16))
