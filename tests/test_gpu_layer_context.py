@@ -354,3 +354,37 @@ def test_profile_counts_what_stands_around_the_layers(b, n):
         assert prof["shared_expert"] == 4 * layers and prof["norm"] == layers + 1 and prof["combine"] == layers and sum(prof.values()) == count
     finally:
         run.close()
+
+
+@pytest.mark.parametrize("n", [1, 4, 20, 200, 600])
+def test_combine_left_to_a_gate_kernel_that_chooses_nothing(b, n):
+    """A layer's combine is left to the next layer's gate kernel; with a registered routing that kernel makes the logits only."""
+    h, e, k, layers = 512, 16, 3, 4
+    w = synth.tiny(n_layers=layers, n_experts=e, top_k=k, hidden=h, intermediate=256)
+    run, one = runner(w, capacity=[6, 16, 3, 9], max_tokens=n), runner(w, capacity=[6, 16, 3, 9], max_tokens=n)
+    try:
+        bias = 0.1 * torch.randn(e, generator=torch.Generator().manual_seed(1)).cuda()
+        for r in (run, one):
+            r.ctx.register_routing(1, b.Routing(e, k, score=b.SCORE_SIGMOID, n_groups=4, top_groups=2, group_top=2, scale=1.5), bias.data_ptr())
+            r.ctx.register_routing(2, b.Routing(e, k))
+        for it in range(3):
+            h_bits, conf = synth.flat_tokens(w, n, 30 + it)
+            x, c = dev(h_bits), torch.from_numpy(conf).cuda()
+            got, out = torch.empty_like(x), torch.empty_like(x)
+            before = run.ctx.launch_count()
+            run.ctx.denoise_iteration(x.data_ptr(), c.data_ptr(), n, got.data_ptr())
+            fused = run.ctx.launch_count() - before
+            before = one.ctx.launch_count()
+            for layer in range(layers):
+                one.step(layer, x, c, out)
+                nxt = torch.empty_like(x)
+                one.ctx.residual_add(x.data_ptr(), out.data_ptr(), nxt.data_ptr(), x.numel())
+                x = nxt
+            single = one.ctx.launch_count() - before
+            torch.cuda.synchronize()
+            assert single - fused >= layers - 1            # (every combine but the last one is another kernel's)
+            assert torch.equal(got.view(torch.int16), x.view(torch.int16))
+            assert (run.ctx.stats().hits, run.ctx.stats().misses) == (one.ctx.stats().hits, one.ctx.stats().misses)
+    finally:
+        run.close()
+        one.close()

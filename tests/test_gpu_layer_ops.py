@@ -745,3 +745,14 @@ def test_products_on_pairs_beside_others(b):
     for o in outs:
         for got, ref in zip(o, want):
             assert torch.equal(got.view(torch.int16), ref.view(torch.int16))
+
+
+@pytest.mark.parametrize("score", [0, 1])
+@pytest.mark.parametrize("e,k,groups,top_groups,group_top", [(32, 32, 1, 1, 1), (7, 7, 1, 1, 1), (64, 32, 8, 4, 2), (256, 32, 8, 1, 1), (256, 32, 8, 1, 2), (60, 30, 4, 2, 1), (17, 17, 17, 17, 1)])
+def test_route_takes_every_expert_that_stays(b, e, k, groups, top_groups, group_top, score):
+    """As many experts wanted as the groups that stay have: nothing is left behind the last choice."""
+    rng = np.random.default_rng(e + k)
+    logits = (2 * rng.normal(size=(300, e))).astype(np.float32)
+    masked = np.where(rng.random(e) < 0.3, -np.inf, 0.1).astype(np.float32)
+    for bias in (None, (0.05 * rng.normal(size=e)).astype(np.float32), masked):
+        check_route(b, logits, bias, top_k=k, score=score, n_groups=groups, top_groups=top_groups, group_top=group_top)
