@@ -390,7 +390,9 @@ int oled_route_noalloc(const void* hidden, const void* w_router, const float* bi
  *          s_e + bias_e (2), and the token's experts come from the top_groups largest groups.
  *   ids    the top_k largest choices, in descending order.  Equal values go to the lower index.  Choices are told apart as
  *          64-bit arithmetic tells them apart, also where fp32 scores are equal.
- *   gate   scale * s / (sum of the chosen s + 1e-20) with renormalise, else scale * s.
+ *   gate   scale * s / (sum of the chosen s + 1e-20) with renormalise, else scale * s.  In fp32: within 2^-19 of itself for
+ *          sigmoids, 2^-17 for softmax scores of logits up to 16 below the largest, 2^-23 more for each unit beyond; what is
+ *          below 2^-126 counts as 0 (before the quotient).
  * A NaN logit counts as -inf, its choice and a choice that is NaN too; the ids of a token stay distinct, also where every
  * choice is -inf. */
 #define OLED_SCORE_SOFTMAX 0
@@ -422,7 +424,7 @@ size_t oled_route_scored_scratch(const oled_routing* routing, int32_t n_tokens);
  *   h  = rms(x_out) * pre_weight, as bf16 (h), as e4m3 codes with a scale per row and 128 columns (h_codes, h_scales;
  *        as oled_quantize_blocks() makes them), both, or, with pre_weight NULL, not at all
  *   rms(v) = v / sqrt(mean(v^2) + eps)
- * Computed in fp32; h is made from the unrounded x_out.  x, y: [n_tokens, hidden]; x and x_out in `residual`'s type, all else bf16.
+ * Computed in fp32 (a row whose sum of squares is beyond fp32 has a norm of zeros); h is made from the unrounded x_out.  x, y: [n_tokens, hidden]; x and x_out in `residual`'s type, all else bf16.
  * gate: one row for every gate_tokens consecutive tokens (a gate per block of a batch), or one for all of them (0).
  * x_out may be NULL.  x_out and h may each be x or y itself (the same address, stride and type). */
 typedef struct {

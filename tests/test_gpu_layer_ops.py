@@ -756,3 +756,45 @@ def test_route_takes_every_expert_that_stays(b, e, k, groups, top_groups, group_
     masked = np.where(rng.random(e) < 0.3, -np.inf, 0.1).astype(np.float32)
     for bias in (None, (0.05 * rng.normal(size=e)).astype(np.float32), masked):
         check_route(b, logits, bias, top_k=k, score=score, n_groups=groups, top_groups=top_groups, group_top=group_top)
+
+
+@pytest.mark.parametrize("renormalise", [0, 1])
+@pytest.mark.parametrize("score", [0, 1])
+@pytest.mark.parametrize("e,groups", [(64, 1), (256, 8), (512, 1)])
+def test_route_weights_by_their_roundings(b, e, groups, score, renormalise):
+    """The weights against the formulas' roundings, each in units of 2^-24 of the value (expf 2 units in the last place: 4, the fast quotient
+    2: 4, an addition or product 1)."""
+    rng = np.random.default_rng(14)
+    logits = (3 * rng.normal(size=(400, e))).astype(np.float32)
+    kw = dict(top_k=8, n_groups=groups, top_groups=max(1, groups // 2), group_top=min(2, groups), scale=2.5)
+    ids, gate, *_ = run_route(b, logits, None, score=score, renormalise=renormalise, **kw)
+    want_ids, want, *_ = lo.route_scored(logits, None, softmax=score == 0, renormalise=bool(renormalise), **kw)
+    assert np.array_equal(ids, want_ids)
+    chosen = np.take_along_axis(logits.astype(np.float64), ids, axis=1)
+    below = logits.max(axis=1, keepdims=True) - chosen      # (a logit minus the largest one, rounded: as many units)
+    if score == 1:
+        units = 9.0                                          # exponential 4, one added 1, quotient 4
+        units += 1 + (9 + 5 + 1 + 4 if renormalise else 0)   # scale; the sum's terms, five additions, 1e-20, quotient
+    elif renormalise:
+        units = (below + 4) + (below.max(axis=1, keepdims=True) + 4 + 5 + 1) + 4 + 1
+    else:
+        # the sum of all: its terms 15 together (a term x below the largest is 3 x + 4 off, and counts by exp(-x)), an addition per
+        # expert of a lane and five
+        units = (below + 4) + (15 + e / 32 + 5) + 4 + 1
+    assert np.all(np.abs(gate - want) <= 1.01 * units * 2.0 ** -24 * want)
+
+
+@pytest.mark.parametrize("h", [512, 333])
+def test_norm_of_rows_beyond_fp32(b, h):
+    """Finite rows whose sum of squares is not an fp32 number: their norms are zeros, their neighbours' what they are."""
+    x = torch.randn(5, h, generator=torch.Generator().manual_seed(3))
+    x[1] *= 1e25
+    x[3, 7] = 3e38
+    w = torch.ones(h, dtype=torch.bfloat16, device=DEV)
+    for residual, kind in ((0, torch.bfloat16), (1, torch.float32)):
+        xd, ho = x.to(kind).to(DEV), torch.full((5, h), 5.0, dtype=torch.bfloat16, device=DEV)
+        shape = b.NormShape(hidden=h, residual=residual, gate_tokens=0, eps=1e-6, residual_scale=1.0, x_stride=h, y_stride=h, gate_stride=h, x_out_stride=h, h_stride=h,
+                            codes_stride=h, scales_stride=-(-h // 128))
+        ok(b, b.norm_residual(shape, ptr(xd), None, None, None, ptr(w), 5, stream(), None, ptr(ho), None, None))
+        rms = (ho.double() ** 2).mean(dim=1).sqrt().cpu()
+        assert not bool(ho[[1, 3]].any()) and bool(((rms[[0, 2, 4]] - 1).abs() <= 2.0 ** -8).all())
