@@ -7,7 +7,7 @@ namespace oled {
 
 inline bool off_boundary(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
-// No array's rows are further apart than this (elements): products of strides and rows stay in 64 bits.
+// No array's rows are further apart than this (elements): the last row's offset stays in 64 bits for every array that memory can hold.
 constexpr int64_t kMaxStride = 1ll << 36;
 inline bool stride_ok(int64_t stride, int64_t width) { return stride >= width && stride <= kMaxStride; }
 
